@@ -209,6 +209,7 @@ def prepare(c, seed):
         s["out"] = torch.empty(T, N, dtype=_T[c["y"]], device="cuda")
     if own:
         s["op"] = _description(s)
+    if own and c["kind"] != "quant":
         s["ws"] = torch.empty(max(s["op"].workspace_size(), 16), dtype=torch.uint8, device="cuda")
     return s
 
@@ -237,14 +238,14 @@ def _ptr(t):
 
 def _run_own(s):
     stream = torch.cuda.current_stream().cuda_stream
+    if s["kind"] == "quant":
+        s["op"].forward(s["x"].data_ptr(), s["q"].data_ptr(), s["scale"].data_ptr(), stream)
+        return s["q"], s["scale"]
     ws, ws_bytes = s["ws"].data_ptr(), s["ws"].numel()
     if s["kind"] == "norm":
         scale = s.get("y_scale")
         s["op"].forward(s["x"].data_ptr(), s["gamma"].data_ptr(), s["beta"].data_ptr(), s["y"].data_ptr(), _ptr(scale), ws, ws_bytes, stream)
         return s["y"] if scale is None else (s["y"], scale)
-    if s["kind"] == "quant":
-        s["op"].forward(s["x"].data_ptr(), s["q"].data_ptr(), s["scale"].data_ptr(), ws, ws_bytes, stream)
-        return s["q"], s["scale"]
     if s["kind"] == "matmul":
         s["op"].forward(s["a"].data_ptr(), s["a_scale"].data_ptr(), s["b"].data_ptr(), s["b_scale"].data_ptr(), _ptr(s["bias_"]),
                         s["out"].data_ptr(), ws, ws_bytes, stream)
