@@ -454,6 +454,141 @@ sc_status_t sparse_conv_plan_candidate(const sparse_conv_plan_t* plan, int32_t i
 sc_status_t sparse_conv_quantize_pow2(const float* x, size_t count, int32_t total_bits,
                                       float saturate_at, int8_t* codes, int32_t* frac_bits);
 
+/* ================================================================================================
+ * Operators of channels-last blocks: what stands between and around the convolutions of a network
+ * whose activations are matrices with one row per position (or token) and one column per channel.
+ *
+ *   sparse_conv_group_norm       group norm with an activation
+ *   sparse_conv_quantize_blocks  values -> 8-bit floats with one scale for each block of 128
+ *   sparse_conv_matmul_blocks    product of two matrices held that way (a pointwise layer)
+ *   sparse_conv_matmul_grouped   the products of a layer of experts: ragged groups of rows
+ *
+ * The group norm and the quantiser write the operand that the products read.  None of them has a
+ * plan: a call takes a description by pointer (read during the call only), device pointers and a
+ * stream, is asynchronous, allocates nothing and may be captured into a graph.  Buffers are borrowed.
+ * Descriptions, pointers and workspaces are checked before anything is launched; a call that is
+ * refused launches nothing.  Zero rows (M, N or S = 0) are no error: the call returns SC_OK.
+ * Distances between rows are in elements of the array's own type.  Outputs must not overlap inputs
+ * but where a function says so, and the rows of an output must not overlap one another.
+ *
+ * Blocks: a matrix of M rows and K columns in SC_ELEM_E4M3 comes with a table of 32-bit scales, one
+ * for each 128 columns of a row (activations) or for each 128 rows x 128 columns (weights); the last
+ * blocks of a row and of the rows may be shorter.  The value of an element is its code times its
+ * block's scale.  Codes are the 8-bit floats with 4 exponent and 3 mantissa bits, largest value 448,
+ * no infinities, one NaN (OCP FP8 "E4M3"). */
+typedef enum { SC_ELEM_F32 = 0, SC_ELEM_F16 = 1, SC_ELEM_BF16 = 2, SC_ELEM_E4M3 = 3 } sc_elem_t;
+
+/* Activations: z, max(z, 0) (NaN stays NaN), z / (1 + exp(-z)). */
+typedef enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_SILU = 2 } sc_act_t;
+
+/* Group norm, channels last: N samples of S positions of C channels, the channels of a sample in G
+ * groups of C / G neighbours; with mean and var over the S * C / G values of a group,
+ *     y[n,s,c] = act( (x[n,s,c] - mean) / sqrt(var + eps) * gamma[c] + beta[c] ).
+ * Statistics and arithmetic are in 32 bits (deviations are summed around a mean, not squares), y is
+ * rounded once.  y_type is x_type, or SC_ELEM_E4M3: then every 128 channels of a position are
+ * quantised as by sparse_conv_quantize_blocks, from the 32-bit values. */
+typedef struct {
+    int32_t N, S, C, G;
+    int32_t x_type;              /* SC_ELEM_F32, _F16, _BF16 */
+    int32_t y_type;              /* x_type or SC_ELEM_E4M3 */
+    int32_t act;                 /* sc_act_t */
+    float eps;                   /* >= 0 */
+    int64_t x_sample, x_row;     /* elements between samples / positions of x (>= 0; 0 repeats one) */
+    int64_t y_sample, y_row;     /* the same of y: y_row >= C, y_sample >= (S - 1) y_row + C */
+    int64_t scale_row;           /* floats between the scales of two positions, >= ceil(C / 128) (E4M3 only) */
+} sc_group_norm_t;
+
+/* Bytes of workspace sparse_conv_group_norm needs for this description (0: none). */
+sc_status_t sparse_conv_group_norm_workspace_size(const sc_group_norm_t* d, size_t* bytes);
+
+/*   x       device, x_type, element-aligned      gamma, beta [C] device f32, either may be NULL (1, 0)
+ *   y       device, y_type (E4M3: y_row a multiple of 16, y 16-byte aligned; the bytes between column C and
+ *           the next multiple of 16 are written with zero codes).  y may be x, with x's type and distances.
+ *   y_scale device f32 [N S][scale_row], E4M3 only
+ * Errors: SC_ERR_NULL, SC_ERR_SHAPE (sizes, G not dividing C, distances), SC_ERR_UNSUPPORTED (types,
+ * activation, eps, alignment), SC_ERR_RANGE (S * C or N * S >= 2^31), SC_ERR_WORKSPACE, SC_ERR_HIP. */
+sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const void* x, const float* gamma, const float* beta,
+                                   void* y, float* y_scale, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Quantisation of a matrix by blocks of `rows` x 128 (rows = 1 or 128): with a the largest magnitude
+ * of a block, or 2^-100 where that is larger (an empty or zero block),
+ *     scale = a / 448,   code = e4m3(x * (448 / a)),
+ * each of the divisions and the product one operation in 32 bits, the code the nearest one, ties to even.
+ * A NaN gets the NaN code and leaves its block's scale to the others; a block with an infinity has an
+ * infinite scale, the NaN code at the infinity and zeros elsewhere (its values are NaN). */
+typedef struct {
+    int32_t M, K;                /* K >= 1 */
+    int32_t rows;                /* 1 or 128 */
+    int32_t x_type;              /* SC_ELEM_F32, _F16, _BF16 */
+    int64_t x_row;               /* elements between rows of x, >= 0 */
+    int64_t q_row;               /* codes between rows of q: a multiple of 16, >= K */
+    int64_t scale_row;           /* floats between rows of scale: >= ceil(K / 128) */
+} sc_quantize_blocks_t;
+
+/*   x device, element-aligned      q device, 16-byte aligned; the codes between column K and the next multiple
+ *   of 16 are written as zeros     scale device f32 [ceil(M / rows)][scale_row]
+ * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (rows, types, alignment), SC_ERR_HIP. */
+sc_status_t sparse_conv_quantize_blocks(const sc_quantize_blocks_t* d, const void* x, void* q, float* scale, void* stream);
+
+/* Product of an M x K matrix of activations and an N x K matrix of weights in blocks:
+ *     y[m,n] = act( sum_b a_scale[m,b] b_scale[n / 128, b] sum_{k in block b} a[m,k] b[n,k]  + bias[n] ),
+ * y rounded once.  M = 1 is the form for single positions.
+ * Precision: blocks are added up in 32 bits.  Inside a block, y_type SC_ELEM_F32 has the exact products of codes
+ * summed in 32 bits too (as 16-bit floats, which hold every code).  16-bit results take the 8-bit matrix
+ * cores at twice the rate: these keep 13 bits below the largest product of those that they add at once, which leaves
+ * an error of about 1.6e-5 of the result where its own rounding is 2e-4 (F16) or 1.6e-3 (BF16). */
+typedef struct {
+    int32_t M, N, K;             /* N, K >= 1 */
+    int32_t y_type;              /* SC_ELEM_F32, _F16, _BF16 */
+    int32_t act;                 /* sc_act_t */
+    int64_t a_row, b_row;        /* codes between rows: multiples of 16, >= K */
+    int64_t y_row;               /* elements between rows of y, >= N */
+    int64_t a_scale_row;         /* floats between rows of a_scale [M][.], >= ceil(K / 128) */
+    int64_t b_scale_row;         /* floats between rows of b_scale [ceil(N / 128)][.], >= ceil(K / 128) */
+} sc_matmul_blocks_t;
+
+sc_status_t sparse_conv_matmul_blocks_workspace_size(const sc_matmul_blocks_t* d, size_t* bytes);
+
+/*   a, b device codes, 16-byte aligned, every row readable up to the next multiple of 16 columns (what lies
+ *        between column K and there is ignored)       bias [N] device f32 or NULL
+ *   y    device, element-aligned
+ * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (types, activation, alignment), SC_ERR_RANGE
+ * (a row of codes of 2^22 bytes or more, a block of 256 rows of y of 2^31 bytes or more), SC_ERR_WORKSPACE, SC_ERR_HIP. */
+sc_status_t sparse_conv_matmul_blocks(const sc_matmul_blocks_t* d, const void* a, const float* a_scale, const void* b,
+                                      const float* b_scale, const float* bias, void* y, void* workspace_dev,
+                                      size_t workspace_bytes, void* stream);
+
+/* Products grouped by expert: the M rows of y fall into E neighbouring groups, group e the rows
+ * offsets[e] .. offsets[e+1] - 1, each multiplied with the weights of its own expert:
+ *     y[i,:] = act( a[index[i],:] b[e]^T + bias[e,:] )            (without an index: a[i,:]).
+ * Sums in 32 bits, y rounded once.  a_type SC_ELEM_E4M3: both operands in blocks, with the precision of
+ * sparse_conv_matmul_blocks; SC_ELEM_F16 and SC_ELEM_BF16: both operands of that type, no scales.
+ * Groups may be empty.  The offsets are read by the kernels only: nothing waits for them on the host.
+ * Rows of y below offsets[0] and from offsets[E] on are not written.  Offsets outside 0 .. M are taken as the
+ * nearest of the two, a group that ends before it begins as empty; with offsets that are not ascending the
+ * rows of y are unspecified.  An index outside 0 .. a_rows - 1 stands for a row of zeros. */
+typedef struct {
+    int32_t M, N, K, E;          /* N, K >= 1, 1 <= E <= 4096 */
+    int32_t a_type;              /* SC_ELEM_F16, _BF16, _E4M3 */
+    int32_t y_type;              /* a_type or SC_ELEM_F32; with E4M3 operands SC_ELEM_F32, _F16, _BF16 */
+    int32_t act;                 /* sc_act_t */
+    int32_t a_rows;              /* rows of a (without an index: >= M) */
+    int64_t a_row, b_row;        /* elements between rows: multiples of 16 bytes, >= K */
+    int64_t b_expert;            /* elements between experts of b: a multiple of 16 bytes */
+    int64_t y_row;               /* elements between rows of y, >= N */
+    int64_t a_scale_row, b_scale_row, b_scale_expert;   /* floats; E4M3 only */
+} sc_matmul_grouped_t;
+
+sc_status_t sparse_conv_matmul_grouped_workspace_size(const sc_matmul_grouped_t* d, size_t* bytes);
+
+/*   a, b device, as for sparse_conv_matmul_blocks     a_scale, b_scale E4M3 only
+ *   index device i32 [M] or NULL     offsets device i32 [E + 1]     bias device f32 [E][N] or NULL
+ * Errors: as sparse_conv_matmul_blocks. */
+sc_status_t sparse_conv_matmul_grouped(const sc_matmul_grouped_t* d, const void* a, const float* a_scale,
+                                       const int32_t* index, const int32_t* offsets, const void* b, const float* b_scale,
+                                       const float* bias, void* y, void* workspace_dev, size_t workspace_bytes,
+                                       void* stream);
+
 const char* sparse_conv_status_string(sc_status_t status);
 
 #ifdef __cplusplus

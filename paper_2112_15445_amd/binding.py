@@ -25,6 +25,11 @@ DTYPES = {"f32": SC_F32, "f16": SC_F16, "i8": SC_I8, "cb4": SC_CB4_I8, "cb4h": S
 SC_VARIANT_AUTO, SC_VARIANT_GATHER, SC_VARIANT_SLAB, SC_VARIANT_DENSE = 0, 1, 2, 3
 SC_STATIC_WORKSPACE_BYTES = 32 << 20
 SC_PATH_SPARSE, SC_PATH_DENSE, SC_PATH_LIBRARY = 0, 1, 2
+SC_ELEM_F32, SC_ELEM_F16, SC_ELEM_BF16, SC_ELEM_E4M3 = 0, 1, 2, 3
+ELEMS = {"f32": SC_ELEM_F32, "f16": SC_ELEM_F16, "bf16": SC_ELEM_BF16, "e4m3": SC_ELEM_E4M3}
+SC_ACT_NONE, SC_ACT_RELU, SC_ACT_SILU = 0, 1, 2
+ACTS = {"none": SC_ACT_NONE, "relu": SC_ACT_RELU, "silu": SC_ACT_SILU}
+BLOCK = 128                        # elements of a row that share a scale
 
 # every symbol include/sparse_conv.h declares
 EXPORTS = [
@@ -34,6 +39,9 @@ EXPORTS = [
     "sparse_conv_forward", "sparse_conv_forward_static", "sparse_conv_plan_autotune", "sparse_conv_autotune_workspace_size", "sparse_conv_plan_dispatch", "sparse_conv_plan_set_path",
     "sparse_conv_plan_num_candidates",
     "sparse_conv_plan_candidate", "sparse_conv_quantize_pow2", "sparse_conv_status_string",
+    "sparse_conv_group_norm_workspace_size", "sparse_conv_group_norm", "sparse_conv_quantize_blocks",
+    "sparse_conv_matmul_blocks_workspace_size", "sparse_conv_matmul_blocks",
+    "sparse_conv_matmul_grouped_workspace_size", "sparse_conv_matmul_grouped",
 ]
 
 
@@ -78,6 +86,29 @@ class sc_plan_info_t(ctypes.Structure):
 
 class sc_epilogue_t(ctypes.Structure):
     _fields_ = [("relu", ctypes.c_int32), ("pool", ctypes.c_int32), ("requant", ctypes.c_int32)]
+
+
+def _fields(i32_before, f32, i32_after, i64):
+    return ([(k, ctypes.c_int32) for k in i32_before] + [(k, ctypes.c_float) for k in f32] +
+            [(k, ctypes.c_int32) for k in i32_after] + [(k, ctypes.c_int64) for k in i64])
+
+
+class sc_group_norm_t(ctypes.Structure):
+    _fields_ = _fields(("N", "S", "C", "G", "x_type", "y_type", "act"), ("eps",), (),
+                       ("x_sample", "x_row", "y_sample", "y_row", "scale_row"))
+
+
+class sc_quantize_blocks_t(ctypes.Structure):
+    _fields_ = _fields(("M", "K", "rows", "x_type"), (), (), ("x_row", "q_row", "scale_row"))
+
+
+class sc_matmul_blocks_t(ctypes.Structure):
+    _fields_ = _fields(("M", "N", "K", "y_type", "act"), (), (), ("a_row", "b_row", "y_row", "a_scale_row", "b_scale_row"))
+
+
+class sc_matmul_grouped_t(ctypes.Structure):
+    _fields_ = _fields(("M", "N", "K", "E", "a_type", "y_type", "act", "a_rows"), (), (),
+                       ("a_row", "b_row", "b_expert", "y_row", "a_scale_row", "b_scale_row", "b_scale_expert"))
 
 
 class SparseConvError(RuntimeError):
@@ -126,6 +157,13 @@ def lib() -> ctypes.CDLL:
     L.sparse_conv_quantize_pow2.argtypes = [vp, sz, i32, ctypes.c_float, vp, P(i32)]
     L.sparse_conv_status_string.argtypes = [ctypes.c_int]
     L.sparse_conv_status_string.restype = ctypes.c_char_p
+    L.sparse_conv_group_norm_workspace_size.argtypes = [P(sc_group_norm_t), P(sz)]
+    L.sparse_conv_group_norm.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.sparse_conv_quantize_blocks.argtypes = [vp, vp, vp, vp, vp]
+    L.sparse_conv_matmul_blocks_workspace_size.argtypes = [P(sc_matmul_blocks_t), P(sz)]
+    L.sparse_conv_matmul_blocks.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.sparse_conv_matmul_grouped_workspace_size.argtypes = [P(sc_matmul_grouped_t), P(sz)]
+    L.sparse_conv_matmul_grouped.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("sparse_conv_plan_destroy", "sparse_conv_status_string"):
             getattr(L, name).restype = ctypes.c_int
@@ -309,6 +347,122 @@ class Plan:
                                                N, ctypes.c_void_p(ws_ptr), ws_bytes,
                                                ctypes.c_void_p(stream)),
                "sparse_conv_plan_autotune")
+
+
+# -------------------------------------------------------------------------------------------------
+# operators of channels-last blocks
+# -------------------------------------------------------------------------------------------------
+def _elem(t) -> int:
+    """SC_ELEM_* of a name ("f16"), a torch dtype or the number itself."""
+    if isinstance(t, int):
+        return t
+    if isinstance(t, str):
+        return ELEMS[t]
+    import torch
+    return {torch.float32: SC_ELEM_F32, torch.float16: SC_ELEM_F16, torch.bfloat16: SC_ELEM_BF16,
+            torch.float8_e4m3fn: SC_ELEM_E4M3}[t]
+
+
+def _code(act) -> int:
+    return ACTS[act] if isinstance(act, str) else int(act)
+
+
+def _up(n: int, to: int) -> int:
+    return -(-n // to) * to
+
+
+class _Operator:
+    """A description in the form that the library reads: same calls as the C ABI."""
+    _name = ""
+
+    def __init__(self, desc):
+        self.desc = desc
+        self._at = ctypes.addressof(desc)      # (the structure lives as long as this object)
+
+    def workspace_size(self) -> int:
+        b = ctypes.c_size_t()
+        name = self._name + "_workspace_size"
+        _check(getattr(lib(), name)(ctypes.byref(self.desc), ctypes.byref(b)), name)
+        return int(b.value)
+
+    def _call(self, *args):
+        for a in args:                         # (see Plan.forward: bytes or str would pass as their address)
+            if not isinstance(a, _ADDRESS):
+                raise TypeError("device pointers, sizes and the stream are integers (or None)")
+        st = getattr(lib(), self._name)(self._at, *args)
+        if st:
+            raise SparseConvError(st, self._name)
+
+
+class GroupNorm(_Operator):
+    """sparse_conv_group_norm: y = act(group norm of x), channels last.  Strides are (sample, position) in
+    elements; left out, x and y are contiguous (codes: rows of the next multiple of 16)."""
+    _name = "sparse_conv_group_norm"
+
+    def __init__(self, N, S, C, G, eps=1e-5, act="none", x_type="f16", y_type=None, x_strides=None, y_strides=None, scale_row=None):
+        xt = _elem(x_type)
+        yt = xt if y_type is None else _elem(y_type)
+        xs = (S * C, C) if x_strides is None else x_strides
+        row = _up(C, 16) if yt == SC_ELEM_E4M3 else C
+        ys = (S * row, row) if y_strides is None else y_strides
+        super().__init__(sc_group_norm_t(N, S, C, G, xt, yt, _code(act), eps, xs[0], xs[1], ys[0], ys[1],
+                                         -(-C // BLOCK) if scale_row is None else scale_row))
+
+    def forward(self, x_ptr: int, gamma_ptr: int, beta_ptr: int, y_ptr: int, scale_ptr: int = 0, ws_ptr: int = 0,
+                ws_bytes: int = 0, stream: int = 0):
+        self._call(x_ptr, gamma_ptr, beta_ptr, y_ptr, scale_ptr, ws_ptr, ws_bytes, stream)
+
+
+class BlockQuantizer(_Operator):
+    """sparse_conv_quantize_blocks: codes and scales of blocks of rows x 128."""
+    _name = "sparse_conv_quantize_blocks"
+
+    def __init__(self, M, K, rows=1, x_type="f16", x_row=None, q_row=None, scale_row=None):
+        super().__init__(sc_quantize_blocks_t(M, K, rows, _elem(x_type), K if x_row is None else x_row,
+                                              _up(K, 16) if q_row is None else q_row,
+                                              -(-K // BLOCK) if scale_row is None else scale_row))
+
+    def workspace_size(self) -> int:
+        return 0
+
+    def forward(self, x_ptr: int, q_ptr: int, scale_ptr: int, stream: int = 0):
+        self._call(x_ptr, q_ptr, scale_ptr, stream)
+
+
+class BlockMatmul(_Operator):
+    """sparse_conv_matmul_blocks: y = act(a b^T + bias) of operands in e4m3 blocks."""
+    _name = "sparse_conv_matmul_blocks"
+
+    def __init__(self, M, N, K, y_type="bf16", act="none", a_row=None, b_row=None, y_row=None, a_scale_row=None, b_scale_row=None):
+        row, kb = _up(K, 16), -(-K // BLOCK)
+        super().__init__(sc_matmul_blocks_t(M, N, K, _elem(y_type), _code(act), row if a_row is None else a_row,
+                                            row if b_row is None else b_row, N if y_row is None else y_row,
+                                            kb if a_scale_row is None else a_scale_row, kb if b_scale_row is None else b_scale_row))
+
+    def forward(self, a_ptr: int, a_scale_ptr: int, b_ptr: int, b_scale_ptr: int, bias_ptr: int, y_ptr: int, ws_ptr: int = 0,
+                ws_bytes: int = 0, stream: int = 0):
+        self._call(a_ptr, a_scale_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
+
+
+class GroupedMatmul(_Operator):
+    """sparse_conv_matmul_grouped: the rows of group e of y = act(a[index] b[e]^T + bias[e])."""
+    _name = "sparse_conv_matmul_grouped"
+
+    def __init__(self, M, N, K, E, a_type="bf16", y_type=None, act="none", a_rows=None, a_row=None, b_row=None, b_expert=None,
+                 y_row=None, a_scale_row=None, b_scale_row=None, b_scale_expert=None):
+        at = _elem(a_type)
+        yt = _elem(y_type) if y_type is not None else SC_ELEM_BF16 if at == SC_ELEM_E4M3 else at
+        row, kb = _up(K, 16 if at == SC_ELEM_E4M3 else 8), -(-K // BLOCK)
+        b_row = row if b_row is None else b_row
+        b_scale_row = kb if b_scale_row is None else b_scale_row
+        super().__init__(sc_matmul_grouped_t(M, N, K, E, at, yt, _code(act), M if a_rows is None else a_rows,
+                                             row if a_row is None else a_row, b_row, N * b_row if b_expert is None else b_expert,
+                                             N if y_row is None else y_row, kb if a_scale_row is None else a_scale_row, b_scale_row,
+                                             -(-N // BLOCK) * b_scale_row if b_scale_expert is None else b_scale_expert))
+
+    def forward(self, a_ptr: int, a_scale_ptr: int, index_ptr: int, offsets_ptr: int, b_ptr: int, b_scale_ptr: int, bias_ptr: int,
+                y_ptr: int, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0):
+        self._call(a_ptr, a_scale_ptr, index_ptr, offsets_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
 
 
 # -------------------------------------------------------------------------------------------------
