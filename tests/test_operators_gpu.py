@@ -266,6 +266,7 @@ MATMUL_SHAPES = [  # M, N, K
     (1, 1, 1), (1, 16, 128), (1, 100, 300), (1, 512, 4096), (1, 2049, 640), (2, 64, 1000), (3, 130, 17), (8, 1024, 512), (15, 200, 129), (16, 256, 2048),
     (17, 257, 256), (32, 96, 1100), (33, 512, 384), (64, 64, 64), (65, 130, 100), (100, 1000, 260), (127, 128, 128), (129, 300, 300),
     (200, 2048, 512), (256, 256, 256), (257, 511, 640), (333, 1000, 1100), (700, 70, 900), (1000, 1030, 129), (2100, 520, 272),
+    (4100, 4100, 272),
 ]
 
 
@@ -343,6 +344,7 @@ def test_matmul_blocks_of_no_rows():
 GROUPS = {  # what each expert gets
     "even": [40, 40, 40, 40], "ragged": [0, 1, 130, 0, 17, 64, 3], "one": [0, 0, 200, 0], "single rows": [1] * 9 + [0] * 7,
     "last": [0, 0, 0, 77], "large": [300, 513, 2], "few": [0, 2, 0, 1, 5], "many": [(7 * e) % 11 for e in range(70)],
+    "thousands": [1500, 0, 2700, 3999],
 }
 
 
@@ -398,7 +400,7 @@ def run_grouped(rng, counts, N, K, a_type, y_type, kind, gather, bias, odd, firs
 def test_matmul_grouped(groups, a_type, y_type):
     counts = GROUPS[groups]
     rng = np.random.default_rng(len(groups) * 31 + sum(counts))
-    for i, (N, K) in enumerate(((64, 128), (130, 200), (257, 520), (1, 1), (512, 1024))):
+    for i, (N, K) in enumerate(((64, 128), (130, 200), (257, 520), (1, 1), (512, 1024)) if groups != "thousands" else ((2060, 200), (2048, 128))):
         if groups == "many" and K > 600:
             continue
         gather, bias, odd = (i + len(counts)) % 2 == 1, i % 3 == 1, i % 2
