@@ -49,6 +49,54 @@ __device__ __forceinline__ uint8_t code1(float a)
     return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_range(a), 0.0f, 0, false);
 }
 
+// Sixteen bytes of x as floats: V values from any element-aligned address, or the first `have` of them and zeros behind.
+template <int ET> constexpr int kVec = 16 / (int)sizeof(Elem<ET>);
+template <int ET> __device__ __forceinline__ v4i load_raw(const Elem<ET>* x)
+{
+    v4i raw;
+    __builtin_memcpy(&raw, x, 16);
+    return raw;
+}
+template <int ET> __device__ __forceinline__ v4i load_raw_part(const Elem<ET>* x, int have)
+{
+    Elem<ET> e[kVec<ET>];
+#pragma unroll
+    for (int i = 0; i < kVec<ET>; ++i) e[i] = i < have ? x[i] : (Elem<ET>)0.0f;
+    v4i raw;
+    __builtin_memcpy(&raw, e, 16);
+    return raw;
+}
+template <int ET> __device__ __forceinline__ void to_floats(v4i raw, float* f)
+{
+    typedef Elem<ET> vec __attribute__((ext_vector_type(kVec<ET>)));
+    const vec v = __builtin_bit_cast(vec, raw);
+#pragma unroll
+    for (int i = 0; i < kVec<ET>; ++i) f[i] = (float)v[i];
+}
+// V floats rounded to the type, stored at any element-aligned address; the first `have` of them.
+template <int ET, int V> __device__ __forceinline__ void store_vec(Elem<ET>* y, const float* f, int have)
+{
+    typedef Elem<ET> vec __attribute__((ext_vector_type(V)));
+    vec v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (Elem<ET>)f[i];
+    if (have >= V) __builtin_memcpy(y, &v, sizeof(v));
+    else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < have) y[i] = v[i];
+    }
+}
+// The V codes of f * up; q on V bytes (zeros of f behind the end of a row become zero codes).
+template <int V> __device__ __forceinline__ void store_codes(uint8_t* q, const float* f, float up)
+{
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = codes4(f[4 * i] * up, f[4 * i + 1] * up, f[4 * i + 2] * up, f[4 * i + 3] * up);
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(q) = w[0];
+}
+
 inline sc_status_t launched() { return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP; }
 
 }  // namespace sc

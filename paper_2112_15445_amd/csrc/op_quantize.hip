@@ -12,43 +12,87 @@ struct QuantArgs {
     int64_t x_row, q_row, s_row;
 };
 
-// One workgroup per block of R x 128 values.
-template <int XT, int R> __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a, int64_t blocks)
+// Blocks of one row: 128 values are 16 bytes each of 16 lanes (two-byte types) or 32 (fp32), so that a wave's load is one run of 1 KB;
+// the magnitude goes round those lanes by shuffles and the values never leave the registers between the two passes over them.
+// Four blocks a lane are under way at once.
+template <int XT> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_t items)
 {
-    __shared__ float red[4];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t item = R == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-    if (item >= blocks) return;
-    const int b = (int)(item % a.KB);
-    const int64_t m0 = item / a.KB * R;
-    const int rows = R == 1 ? 1 : (int)min((int64_t)R, a.M - m0);
-    const int c0 = b * kQBlock + lane * 2;
-    const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x);
-    float amax = kAmaxFloor;
-    for (int r = R == 1 ? 0 : wave; r < rows; r += 4)
-        for (int i = 0; i < 2; ++i)
-            if (c0 + i < a.K) amax = fmaxf(amax, fabsf((float)x[(m0 + r) * a.x_row + c0 + i]));
-    for (int o = 32; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-    if constexpr (R > 1) {
-        if (lane == 0) red[wave] = amax;
-        __syncthreads();
-        amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    constexpr int V = kVec<XT>, L = kQBlock / V, U = 4;
+    const int part = threadIdx.x % L;
+    const uint32_t first = blockIdx.x * (256 / L * U) + threadIdx.x / L;
+    v4i raw[U];
+    uint32_t row[U];
+    int col[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t item = min(first + u * (256 / L), items - 1);
+        row[u] = item / (uint32_t)a.KB;
+        col[u] = (int)(item - row[u] * (uint32_t)a.KB) * kQBlock + part * V;
+        const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + row[u] * a.x_row + col[u];
+        raw[u] = col[u] + V <= a.K ? load_raw<XT>(x) : load_raw_part<XT>(x, a.K - col[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[V], amax = kAmaxFloor;
+        to_floats<XT>(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+        if (first + u * (256 / L) >= items) continue;
+        if (col[u] < ((a.K + 15) & ~15)) store_codes<V>(a.q + row[u] * a.q_row + col[u], f, kCodeMax / amax);
+        if (part == 0) a.scale[row[u] * a.s_row + col[u] / kQBlock] = amax / kCodeMax;
+    }
+}
+
+// Blocks of 128 rows: one workgroup each, the whole block in its registers (32 bytes a lane and two-byte type, 64 in fp32).
+template <int XT> __global__ __launch_bounds__(1024) void quantize_tiles_kernel(QuantArgs a)
+{
+    constexpr int V = kVec<XT>, L = kQBlock / V, R = 1024 / L, U = kQBlock / R;   // lanes of a row, rows at once, rows of a lane
+    __shared__ float red[16];
+    const int part = threadIdx.x % L;
+    const uint32_t tile_row = blockIdx.x / (uint32_t)a.KB, b = blockIdx.x - tile_row * (uint32_t)a.KB;
+    const int col = (int)b * kQBlock + part * V;
+    const int m0 = (int)tile_row * kQBlock + threadIdx.x / L;
+    v4i raw[U];
+    float amax = kAmaxFloor;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int m = m0 + u * R;
+        const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + m * a.x_row + col;
+        raw[u] = v4i{0, 0, 0, 0};
+        if (m < a.M) raw[u] = col + V <= a.K ? load_raw<XT>(x) : load_raw_part<XT>(x, a.K - col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[V];
+        to_floats<XT>(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) amax = fmaxf(amax, red[i]);
     const float up = kCodeMax / amax;
-    for (int r = R == 1 ? 0 : wave; r < rows; r += 4)
-        for (int i = 0; i < 2; ++i)
-            if (c0 + i < ((a.K + 15) & ~15)) {
-                const float v = c0 + i < a.K ? (float)x[(m0 + r) * a.x_row + c0 + i] : 0.0f;
-                a.q[(m0 + r) * a.q_row + c0 + i] = code1(v * up);
-            }
-    if (lane == 0 && (R == 1 || wave == 0)) a.scale[item / a.KB * a.s_row + b] = amax / kCodeMax;
+    if (col < ((a.K + 15) & ~15))
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int m = m0 + u * R;
+            float f[V];
+            to_floats<XT>(raw[u], f);
+            if (m < a.M) store_codes<V>(a.q + m * a.q_row + col, f, up);
+        }
+    if (threadIdx.x == 0) a.scale[tile_row * a.s_row + b] = amax / kCodeMax;
 }
 
 template <int XT> sc_status_t launch_quantize(const QuantArgs& a, int rows, hipStream_t stream)
 {
     const int64_t blocks = ceil_div(a.M, rows) * a.KB;
-    if (rows == 1) quantize_kernel<XT, 1><<<dim3((unsigned)ceil_div(blocks, 4)), 256, 0, stream>>>(a, blocks);
-    else quantize_kernel<XT, 128><<<dim3((unsigned)blocks), 256, 0, stream>>>(a, blocks);
+    if (rows == 1) quantize_rows_kernel<XT><<<dim3((unsigned)ceil_div(blocks, 256 / (kQBlock / kVec<XT>) * 4)), 256, 0, stream>>>(a, (uint32_t)blocks);
+    else quantize_tiles_kernel<XT><<<dim3((unsigned)blocks), 1024, 0, stream>>>(a);
     return launched();
 }
 
@@ -62,7 +106,7 @@ extern "C" sc_status_t sparse_conv_quantize_blocks(const sc_quantize_blocks_t* d
     if (!d) return SC_ERR_NULL;
     if (d->M < 0 || d->K <= 0 || d->x_row < 0 || d->q_row < d->K || d->scale_row < ceil_div(d->K, kQBlock)) return SC_ERR_SHAPE;
     if ((d->rows != 1 && d->rows != kQBlock) || !is_wide(d->x_type) || d->q_row % 16) return SC_ERR_UNSUPPORTED;
-    if (ceil_div(d->M, d->rows) * ceil_div(d->K, kQBlock) >= (int64_t)1 << 31) return SC_ERR_RANGE;
+    if (ceil_div(d->M, d->rows) * ceil_div(d->K, kQBlock) >= (int64_t)1 << (d->rows == 1 ? 27 : 22)) return SC_ERR_RANGE;   // threads of a launch
     if (d->M == 0) return SC_OK;
     if (!x || !q || !scale) return SC_ERR_NULL;
     if (!aligned(x, elem_bytes(d->x_type)) || !aligned(q, 16) || !aligned(scale, 4)) return SC_ERR_UNSUPPORTED;
