@@ -378,6 +378,7 @@ class _Operator:
     def __init__(self, desc):
         self.desc = desc
         self._at = ctypes.addressof(desc)      # (the structure lives as long as this object)
+        self._fn = getattr(lib(), self._name)
 
     def workspace_size(self) -> int:
         b = ctypes.c_size_t()
@@ -385,13 +386,12 @@ class _Operator:
         _check(getattr(lib(), name)(ctypes.byref(self.desc), ctypes.byref(b)), name)
         return int(b.value)
 
-    def _call(self, *args):
-        for a in args:                         # (see Plan.forward: bytes or str would pass as their address)
-            if not isinstance(a, _ADDRESS):
-                raise TypeError("device pointers, sizes and the stream are integers (or None)")
-        st = getattr(lib(), self._name)(self._at, *args)
-        if st:
-            raise SparseConvError(st, self._name)
+    def _refused(self, status):
+        raise SparseConvError(status, self._name)
+
+
+# (In every forward: addresses, sizes and the stream are integers, 0 for none; the alternation of all of them is a TypeError for
+# anything else, bytes and str among it, which ctypes would pass as their address.)
 
 
 class GroupNorm(_Operator):
@@ -410,7 +410,10 @@ class GroupNorm(_Operator):
 
     def forward(self, x_ptr: int, gamma_ptr: int, beta_ptr: int, y_ptr: int, scale_ptr: int = 0, ws_ptr: int = 0,
                 ws_bytes: int = 0, stream: int = 0):
-        self._call(x_ptr, gamma_ptr, beta_ptr, y_ptr, scale_ptr, ws_ptr, ws_bytes, stream)
+        x_ptr | gamma_ptr | beta_ptr | y_ptr | scale_ptr | ws_ptr | ws_bytes | stream
+        status = self._fn(self._at, x_ptr, gamma_ptr, beta_ptr, y_ptr, scale_ptr, ws_ptr, ws_bytes, stream)
+        if status:
+            self._refused(status)
 
 
 class BlockQuantizer(_Operator):
@@ -426,7 +429,10 @@ class BlockQuantizer(_Operator):
         return 0
 
     def forward(self, x_ptr: int, q_ptr: int, scale_ptr: int, stream: int = 0):
-        self._call(x_ptr, q_ptr, scale_ptr, stream)
+        x_ptr | q_ptr | scale_ptr | stream
+        status = self._fn(self._at, x_ptr, q_ptr, scale_ptr, stream)
+        if status:
+            self._refused(status)
 
 
 class BlockMatmul(_Operator):
@@ -441,7 +447,10 @@ class BlockMatmul(_Operator):
 
     def forward(self, a_ptr: int, a_scale_ptr: int, b_ptr: int, b_scale_ptr: int, bias_ptr: int, y_ptr: int, ws_ptr: int = 0,
                 ws_bytes: int = 0, stream: int = 0):
-        self._call(a_ptr, a_scale_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
+        a_ptr | a_scale_ptr | b_ptr | b_scale_ptr | bias_ptr | y_ptr | ws_ptr | ws_bytes | stream
+        status = self._fn(self._at, a_ptr, a_scale_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
+        if status:
+            self._refused(status)
 
 
 class GroupedMatmul(_Operator):
@@ -462,7 +471,10 @@ class GroupedMatmul(_Operator):
 
     def forward(self, a_ptr: int, a_scale_ptr: int, index_ptr: int, offsets_ptr: int, b_ptr: int, b_scale_ptr: int, bias_ptr: int,
                 y_ptr: int, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0):
-        self._call(a_ptr, a_scale_ptr, index_ptr, offsets_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
+        a_ptr | a_scale_ptr | index_ptr | offsets_ptr | b_ptr | b_scale_ptr | bias_ptr | y_ptr | ws_ptr | ws_bytes | stream
+        status = self._fn(self._at, a_ptr, a_scale_ptr, index_ptr, offsets_ptr, b_ptr, b_scale_ptr, bias_ptr, y_ptr, ws_ptr, ws_bytes, stream)
+        if status:
+            self._refused(status)
 
 
 # -------------------------------------------------------------------------------------------------

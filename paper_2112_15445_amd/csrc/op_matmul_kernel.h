@@ -12,9 +12,13 @@
 // The 16 weight rows of a matrix operand are picked so that a lane ends up with eight neighbouring columns of y over two
 // products (n = 32 (i/2) + 8 (r/4) + 4 (i%2) + r%4 for row r of product i): stores are 16 bytes wide.
 //
-// LDS: a row's eight 16-byte chunks are stored at chunk ^ key(row), with keys under which the 16 rows of an operand read from
-// eight different places: no two lanes of a read that are served together meet in a bank.
+// LDS: a row's eight 16-byte chunks are stored at chunk ^ key(row).  A 16-byte read of a wave is served in four turns of sixteen lanes
+// over the 64 banks (two rows): lanes 0-3, 12-15 and 20-27 together, 4-11 with 16-19 and 28-31, and the same 32 lanes on.  Of an
+// operand's rows c = lane % 16 a turn has each once, c = 0-3 and 12-15 with one chunk and 4-11 with its neighbour but one
+// (chunks 2 q + h, q = lane / 16): keys 0-3 for the former and 4-7 for the latter put all of them in banks of their own.
 #pragma once
+
+#include <type_traits>
 
 #include "op_common.h"
 
@@ -42,18 +46,14 @@ struct MatmulArgs {
 
 constexpr int kSlab = 128;                   // bytes of a row that are staged at a time
 
-// The 16 bytes of a row that begin at `at`, zeros behind the end of the row.
-__device__ __forceinline__ v4i row_chunk(const uint8_t* row, int at, int kbytes)
+// The first `have` bytes of a chunk (all of them from 16 on), zeros behind.
+__device__ __forceinline__ v4i first_bytes(v4i v, int have)
 {
-    v4i v = {0, 0, 0, 0};
-    if (at >= kbytes) return v;
-    v = *reinterpret_cast<const v4i*>(row + at);
-    const int have = kbytes - at;
-    if (have < 16)
-        for (int i = 0; i < 4; ++i) {
-            const int h = have - 4 * i;
-            v[i] = h <= 0 ? 0 : h >= 4 ? v[i] : v[i] & ((1 << (8 * h)) - 1);
-        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int h = have - 4 * i;
+        v[i] = h <= 0 ? 0 : h >= 4 ? v[i] : v[i] & ((1 << (8 * h)) - 1);
+    }
     return v;
 }
 
@@ -109,7 +109,7 @@ template <int BT> __device__ __forceinline__ bool find_group(const MatmulArgs& p
         const uint64_t behind = __ballot(tile < upto);
         if (behind) {
             const int at = __builtin_ctzll(behind);
-            e = base + at;
+            e = __builtin_amdgcn_readfirstlane(base + at);
             m0 = __builtin_amdgcn_readfirstlane(__shfl(lo + (tile - (upto - t)) * BT, at));
             hi_ = __builtin_amdgcn_readfirstlane(__shfl(hi, at));
             return true;
@@ -120,39 +120,90 @@ template <int BT> __device__ __forceinline__ bool find_group(const MatmulArgs& p
 }
 
 // One 16-byte (or 4-byte) direct-to-LDS load a lane: lane i's bytes go to `lds` + i * width.  Written by hand so that the compiler does
-// not make the reads of the other buffer wait for it; the caller waits on vmcnt itself.
+// not make the reads of the other buffer wait for it; the caller waits on vmcnt itself (staged()), which is also what keeps reads of
+// the buffer behind it.
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
+{
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
 template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint32_t lds)
 {
     uint32_t keep;
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(off), "s"(base), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(off), "s"(base), "s"(lds));
     else
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(off), "s"(base), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(off), "s"(base), "s"(lds));
 }
 template <int BYTES> __device__ __forceinline__ void to_lds_ptr(const uint8_t* src, uint32_t lds)
 {
     uint32_t keep;
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(src), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(src), "s"(lds));
     else
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(src), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0" : "=&s"(keep) : "v"(src), "s"(lds));
 }
 
-__device__ __forceinline__ int token_key(int row) { return row & 7; }
-__device__ __forceinline__ int weight_key(int row) { return (row & 3) | ((row >> 1) & 4); }
+// key of the row that lane c of sixteen reads
+__device__ __forceinline__ int lane_key(int c) { return ((c >> 1) & 1) | ((c >> 2) & 2) | (((c >> 2) ^ (c >> 1)) & 2) << 1; }
+__device__ __forceinline__ int token_key(int row) { return lane_key(row & 15); }
+__device__ __forceinline__ int weight_key(int row) { return lane_key((row & 3) | ((row >> 1) & 12)); }
 
-// BT x BN of y per workgroup, WT x WN waves.  AT: type of the operands, YT: of y.
-template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN>
+// One block's product of codes, unscaled: 16 weight rows (x) and 16 rows of a (z).
+template <int YT> __device__ __forceinline__ v4f block_product(const v4i* x, const v4i* z)
+{
+    v4f d = {0, 0, 0, 0};
+    if constexpr (YT == SC_ELEM_F32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(x[h][2 * u], x[h][2 * u + 1]), widen8(z[h][2 * u], z[h][2 * u + 1]), d, 0, 0, 0);
+    } else {
+        d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7),
+                                                             __builtin_shufflevector(z[0], z[1], 0, 1, 2, 3, 4, 5, 6, 7), d, 0, 0, 0, 0, 0, 0);
+    }
+    return d;
+}
+
+// acc += one slab's product of 16 weight rows (x) and 16 rows of a (z); codes: times the scale of the block.
+template <int AT, int YT> __device__ __forceinline__ void multiply(v4f& acc, const v4i* x, const v4i* z, float scale)
+{
+    if constexpr (AT == SC_ELEM_E4M3) {
+        const v4f d = block_product<YT>(x, z);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[v] += scale * d[v];
+    } else {
+        (void)scale;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if constexpr (AT == SC_ELEM_F16) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x[h]), __builtin_bit_cast(v8h, z[h]), acc, 0, 0, 0);
+            else acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, x[h]), __builtin_bit_cast(v8b, z[h]), acc, 0, 0, 0);
+    }
+}
+
+// Waits until at most N of this wave's copies are under way, then for the other waves.
+template <int N> __device__ __forceinline__ void staged()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// BT x BN of y per workgroup, WT x WN waves, ST slabs in LDS: one is multiplied while the ST - 1 behind it arrive.
+// AT: type of the operands, YT: of y.
+template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN, int ST>
 __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs p)
 {
     constexpr int W = WT * WN, TF = BT / WT / 16, NF = BN / WN / 16;    // waves; 16-row products of a wave along the rows / columns of y
     constexpr int AI = BT / 8 / W, BI = BN / 8 / W;                     // copies of 1 KB (eight rows) a wave makes of a slab
     constexpr bool CODES = AT == SC_ELEM_E4M3;
     constexpr int kStage = (BT + BN) * kSlab, kScales = CODES ? W * 64 * 4 : 0;
+    constexpr int kCopies = AI + BI + (CODES ? 1 : 0);                  // of a wave and slab
     static_assert(AI * 8 * W == BT && BI * 8 * W == BN && NF % 2 == 0, "tile");
     static_assert(!CODES || (BT + (BN + 127) / 128 <= W * 64), "one lane fetches a scale");
-    __shared__ __align__(16) uint8_t lds[2 * (kStage + kScales)];
+    __shared__ __align__(16) uint8_t lds[ST * (kStage + kScales)];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntn = (p.N + BN - 1) / BN;
 
@@ -167,7 +218,8 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
         id = xcd * each + min(xcd, more) + at;
     }
     const int band = id / (8 * ntn), inband = id - band * 8 * ntn, height = min(8, ntm - band * 8);
-    const int tm = band * 8 + inband % height, tn = inband / height;
+    // (divisions are done in vector registers; what comes of these is the same in every lane and belongs in scalar ones)
+    const int tn = __builtin_amdgcn_readfirstlane(inband / height), tm = __builtin_amdgcn_readfirstlane(band * 8 + inband - tn * height);
     int e = 0, m0 = tm * BT, hi = p.M;
     if constexpr (GROUPED)
         if (!find_group<BT>(p, tm, e, m0, hi)) return;
@@ -215,21 +267,28 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
 
     // Slabs: a last, short one comes first (it is masked on its way through registers), then the whole ones in their order.
     const int whole = p.kbytes / kSlab, tail = p.kbytes % kSlab, slabs = whole + (tail != 0);
-    auto stage = [&](int s, int buf) {       // whole slab s
+    auto copy = [&](int i, int s, int buf) {  // copy i of whole slab s
         const uint32_t at = lds0 + buf * kStage;
-#pragma unroll
-        for (int i = 0; i < AI; ++i)
-            if constexpr (GROUPED) to_lds_ptr<16>(aptr[i] + s * kSlab, at + (wave + i * W) * 1024);
-            else to_lds<16>(abase + s * kSlab, aoff[i], at + (wave + i * W) * 1024);
-#pragma unroll
-        for (int i = 0; i < BI; ++i) to_lds<16>(bbase + s * kSlab, boff[i], at + BT * kSlab + (wave + i * W) * 1024);
-        if constexpr (CODES) to_lds_ptr<4>(sptr + s * 4, lds0 + 2 * kStage + buf * kScales + wave * 256);
+        if (i < BI) to_lds<16>(uniform(bbase + s * kSlab), boff[i], at + BT * kSlab + (wave + i * W) * 1024);
+        else if (i < BI + AI) {
+            const int j = i - BI;
+            if constexpr (GROUPED) to_lds_ptr<16>(aptr[j] + s * kSlab, at + (wave + j * W) * 1024);
+            else to_lds<16>(uniform(abase + s * kSlab), aoff[j], at + (wave + j * W) * 1024);
+        } else to_lds_ptr<4>(sptr + s * 4, lds0 + ST * kStage + buf * kScales + wave * 256);
     };
+    auto stage = [&](int s, int buf) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy(i, s, buf);
+    };
+    const int ahead = min(ST - 1, slabs);
     if (tail) {
+        v4i part[AI + BI];
+        int have[AI + BI];                   // bytes of the short slab from a lane's chunk on
+        float scale = 0.0f;
+#pragma unroll
         for (int i = 0; i < AI + BI; ++i) {
             const bool of_a = i < AI;
-            const int j = of_a ? i : i - AI;
-            const int r = (wave + j * W) * 8 + (lane >> 3);
+            const int r = (wave + (of_a ? i : i - AI) * W) * 8 + (lane >> 3);
             const int chunk = ((lane & 7) ^ (of_a ? token_key(r) : weight_key(r))) << 4;
             const uint8_t* row;
             if (of_a) {
@@ -239,101 +298,218 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             } else {
                 row = bbase + min(r, p.N - 1 - n0) * p.b_row;
             }
-            *reinterpret_cast<v4i*>(lds + (of_a ? 0 : BT * kSlab) + (wave + j * W) * 1024 + lane * 16) = row_chunk(row + whole * kSlab, chunk, tail);
+            have[i] = tail - chunk;
+            part[i] = v4i{0, 0, 0, 0};
+            if (have[i] > 0) part[i] = *reinterpret_cast<const v4i*>(row + whole * kSlab + chunk);
         }
-        if constexpr (CODES) *reinterpret_cast<float*>(lds + 2 * kStage + tid * 4) = *reinterpret_cast<const float*>(sptr + whole * 4);
+        if constexpr (CODES) scale = *reinterpret_cast<const float*>(sptr + whole * 4);
+        for (int s = 1; s < ahead; ++s) stage(s - 1, s);
+#pragma unroll
+        for (int i = 0; i < AI + BI; ++i) {
+            const bool of_a = i < AI;
+            *reinterpret_cast<v4i*>(lds + (of_a ? 0 : BT * kSlab) + (wave + (of_a ? i : i - AI) * W) * 1024 + lane * 16) = first_bytes(part[i], have[i]);
+        }
+        if constexpr (CODES) *reinterpret_cast<float*>(lds + ST * kStage + tid * 4) = scale;
     } else {
-        stage(0, 0);
+        for (int s = 0; s < ahead; ++s) stage(s, s);
     }
 
     const int wt = wave % WT, wn = wave / WT;
     const int c = lane & 15, q = lane >> 4;
     // This lane's places in a slab: token row c of a product, weight row 8 (c/4) + c%4 of a pair of products.
+    const int key = lane_key(c);
     const int trow = wt * (TF * 16) + c, wrow = wn * (NF * 16) + (c >> 2) * 8 + (c & 3);
     v4f acc[NF][TF] = {};
-    for (int it = 0; it < slabs; ++it) {
-        const int buf = it & 1;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (it + 1 < slabs) stage(tail ? it : it + 1, buf ^ 1);
+    // A slab is NF steps: one operand of the weights against the TF of a.  The weights are read two steps ahead, and a block's sums
+    // are scaled and added under the matrix instructions of the step behind it.
+    int buf = 0, next = (ST - 1) % ST;
+    // Slab `it`; MORE: the copies of slab it + ST - 1 are made in its first steps (a wave that issues them all at once waits for the
+    // others', and late ones hold up the next slab).
+    auto slab = [&](auto more, int it) {
+        constexpr bool MORE = decltype(more)::value;
+        constexpr int kSpread = NF > 2 ? NF / 2 : NF;
+        const int coming = it + ST - 1 - (tail != 0);
         const uint8_t* A = lds + buf * kStage;
         const uint8_t* Bm = A + BT * kSlab;
-        const float* S = reinterpret_cast<const float*>(lds + 2 * kStage + buf * kScales);
-        v4i t[TF][2];
-        float sc[TF];
+        v4i t[TF][2], w[3][2];
+        v4f d[2][TF];
+        float sc[TF], sw = 0.0f;
+        auto read_w = [&](int i) {
+            const int r = wrow + (i >> 1) * 32 + (i & 1) * 4;
 #pragma unroll
-        for (int j = 0; j < TF; ++j) {
-            const int r = trow + 16 * j;
+            for (int h = 0; h < 2; ++h) w[i % 3][h] = *reinterpret_cast<const v4i*>(Bm + r * kSlab + (((2 * q + h) ^ key) << 4));
+        };
+        auto add = [&](int i, int j) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) t[j][h] = *reinterpret_cast<const v4i*>(A + r * kSlab + (((2 * q + h) ^ token_key(r)) << 4));
-            if constexpr (CODES) sc[j] = S[r] * S[BT + (wn * NF * 16) / 128];
+            for (int v = 0; v < 4; ++v) acc[i][j][v] += sc[j] * d[i & 1][j][v];
+        };
+        read_w(0);
+#pragma unroll
+        for (int j = 0; j < TF; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) t[j][h] = *reinterpret_cast<const v4i*>(A + (trow + 16 * j) * kSlab + (((2 * q + h) ^ key) << 4));
+        if (NF > 1) read_w(1);
+        if constexpr (CODES) {
+            const float* S = reinterpret_cast<const float*>(lds + ST * kStage + buf * kScales);
+            sw = S[BT + (wn * NF * 16) / 128];
+#pragma unroll
+            for (int j = 0; j < TF; ++j) sc[j] = S[trow + 16 * j];
         }
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
-            const int r = wrow + (i >> 1) * 32 + (i & 1) * 4;
-            v4i w[2];
+            if (i + 2 < NF) read_w(i + 2);
+            if constexpr (MORE)
+                if (i < kSpread)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w[h] = *reinterpret_cast<const v4i*>(Bm + r * kSlab + (((2 * q + h) ^ weight_key(r)) << 4));
+                    for (int u = i * kCopies / kSpread; u < (i + 1) * kCopies / kSpread; ++u) copy(u, coming, next);
+            if (CODES && i == 1)
+#pragma unroll
+                for (int j = 0; j < TF; ++j) sc[j] *= sw;
 #pragma unroll
             for (int j = 0; j < TF; ++j) {
-                if constexpr (CODES && YT == SC_ELEM_F32) {
-                    v4f d = {0, 0, 0, 0};
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(w[h][2 * u], w[h][2 * u + 1]), widen8(t[j][h][2 * u], t[j][h][2 * u + 1]), d, 0, 0, 0);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][j][v] += sc[j] * d[v];
-                } else if constexpr (CODES) {
-                    const v8i x = __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    const v8i z = __builtin_shufflevector(t[j][0], t[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    const v4f d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, z, v4f{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][j][v] += sc[j] * d[v];
+                if constexpr (CODES) {
+                    d[i & 1][j] = block_product<YT>(w[i % 3], t[j]);
+                    if (i > 0) add(i - 1, j);
                 } else {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        if constexpr (AT == SC_ELEM_F16)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w[h]), __builtin_bit_cast(v8h, t[j][h]), acc[i][j], 0, 0, 0);
-                        else
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, w[h]), __builtin_bit_cast(v8b, t[j][h]), acc[i][j], 0, 0, 0);
+                    multiply<AT, YT>(acc[i][j], w[i % 3], t[j], 0.0f);
                 }
             }
+            // In the widest tile: the reads first, then the scaling of one product under each matrix instruction (245 us against 252 at
+            // 8192 x 8192 x 4096; narrower tiles lose by it).
+            if (CODES && YT != SC_ELEM_F32 && NF == 8 && i > 0) {
+                if (i + 2 < NF) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int j = 0; j < TF; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (CODES)
+#pragma unroll
+            for (int j = 0; j < TF; ++j) add(NF - 1, j);
+        buf = buf + 1 == ST ? 0 : buf + 1;
+        next = next + 1 == ST ? 0 : next + 1;
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    int it = 0;
+    for (; it + ST - 1 < slabs; ++it) {
+        staged<(ST - 2) * kCopies>();
+        slab(yes, it);
+    }
+    for (; it < slabs; ++it) {
+        staged<0>();
+        slab(no, it);
     }
 
     // y: a lane has eight neighbouring columns per pair of products.
     const bool wide = (reinterpret_cast<uintptr_t>(p.y) & 15) == 0 && (p.y_row * (int64_t)sizeof(Elem<YT>)) % 16 == 0;
     const float* bias = p.bias ? p.bias + (GROUPED ? (int64_t)e * p.N : 0) : nullptr;
+    bool zero[TF] = {};
+    if constexpr (GROUPED)
+        if (p.index)
 #pragma unroll
-    for (int j = 0; j < TF; ++j) {
-        const int r = wt * (TF * 16) + 16 * j + c;
-        if (r >= rows) continue;
-        bool zero = false;
-        if constexpr (GROUPED) zero = p.index && (uint32_t)p.index[m0 + r] >= (uint32_t)p.a_rows;
-        Elem<YT>* y = static_cast<Elem<YT>*>(p.y) + (int64_t)(m0 + r) * p.y_row;
+            for (int j = 0; j < TF; ++j) zero[j] = (uint32_t)p.index[m0 + min(trow + 16 * j, rows - 1)] >= (uint32_t)p.a_rows;
 #pragma unroll
-        for (int i = 0; i < NF; i += 2) {
-            const int n = n0 + wn * (NF * 16) + (i >> 1) * 32 + q * 8;
-            if (n >= p.N) continue;
-            typedef Elem<YT> v8y __attribute__((ext_vector_type(8)));
-            v8y out;
+    for (int i = 0; i < NF; i += 2) {
+        const int n = n0 + wn * (NF * 16) + (i >> 1) * 32 + q * 8;
+        if (n >= p.N) continue;
+        const bool whole8 = n + 8 <= p.N;
+        float add[8] = {};
+        if (bias) {
+            if (whole8) {
+                __builtin_memcpy(add, bias + n, 32);
+            } else {
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                float z = zero ? 0.0f : acc[i + (v >> 2)][j][v & 3];
-                if (bias) z += bias[min(n + v, p.N - 1)];
-                out[v] = (Elem<YT>)act_of(z, p.act);
+                for (int v = 0; v < 8; ++v) add[v] = bias[min(n + v, p.N - 1)];
             }
-            if (wide && n + 8 <= p.N) {
-                *reinterpret_cast<v8y*>(y + n) = out;
+        }
+#pragma unroll
+        for (int j = 0; j < TF; ++j) {
+            const int r = trow + 16 * j;
+            if (r >= rows) continue;
+            Elem<YT>* y = static_cast<Elem<YT>*>(p.y) + (int64_t)(m0 + r) * p.y_row + n;
+            float z[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) z[v] = act_of((zero[j] ? 0.0f : acc[i + (v >> 2)][j][v & 3]) + add[v], p.act);
+            if (wide) {
+                store_vec<YT, 8>(y, z, p.N - n);
             } else {
 #pragma unroll
                 for (int v = 0; v < 8; ++v)
-                    if (n + v < p.N) y[n + v] = out[v];
+                    if (n + v < p.N) y[v] = (Elem<YT>)z[v];
             }
         }
+    }
+}
+
+// Few rows: 16 of them against 16 columns a workgroup, whose waves share the summed dimension out among themselves.
+// Bound by reading the weights once: they go from memory into the registers that multiply them (a lane reads 16 bytes of its
+// row, four lanes 64 in a row), kAtOnce slabs of a wave under way together, and the waves' sums meet in LDS, in their order.
+constexpr int kAtOnce = 4;
+template <int AT, int YT, bool GROUPED> __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs p)
+{
+    constexpr bool CODES = AT == SC_ELEM_E4M3;
+    extern __shared__ __align__(16) v4f part[];          // [waves][64]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int ntn = (p.N + 15) / 16, tm = blockIdx.x / ntn, n0 = (blockIdx.x - tm * ntn) * 16;
+    int e = 0, m0 = tm * 16, hi = p.M;
+    if constexpr (GROUPED)
+        if (!find_group<16>(p, tm, e, m0, hi)) return;
+    const int rows = min(16, hi - m0), c = lane & 15, q = lane >> 4;
+    const uint8_t* w = p.b + (GROUPED ? e * p.b_expert : 0) + min(n0 + c, p.N - 1) * p.b_row + q * 16;
+    const float* bs = CODES ? p.bs + (GROUPED ? e * p.bs_expert : 0) + n0 / kQBlock * p.bs_row : nullptr;
+    int m = m0 + min(c, rows - 1);
+    if (GROUPED && p.index) m = p.index[m];
+    const bool real = (uint32_t)m < (uint32_t)p.a_rows;      // (an index that stands for zeros: see the tile)
+    const uint8_t* t = (real ? p.a + m * p.a_row : p.b) + q * 16;
+    const float* as = CODES ? real ? p.as + m * p.as_row : p.bs : nullptr;
+    const int slabs = (p.kbytes + kSlab - 1) / kSlab;
+    v4f acc = {0, 0, 0, 0};
+    auto some = [&](int s0, bool whole) {
+        v4i x[kAtOnce][2], z[kAtOnce][2];
+        float sc[kAtOnce], sb[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = (s0 + u * waves) * kSlab + 64 * h, have = p.kbytes - at - q * 16;
+                x[u][h] = v4i{0, 0, 0, 0};
+                if (whole || have > 0) x[u][h] = *reinterpret_cast<const v4i*>(w + at);
+                if (!whole) x[u][h] = first_bytes(x[u][h], have);
+                z[u][h] = v4i{0, 0, 0, 0};
+                if (whole || have > 0) z[u][h] = *reinterpret_cast<const v4i*>(t + at);
+                if (!whole) z[u][h] = first_bytes(z[u][h], have);
+            }
+            if constexpr (CODES) {
+                const int kb = whole ? s0 + u * waves : min(s0 + u * waves, slabs - 1);
+                sb[u] = bs[kb];
+                sc[u] = as[kb];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (!whole && s0 + u * waves >= slabs) break;
+            multiply<AT, YT>(acc, x[u], z[u], CODES ? sc[u] * sb[u] : 0.0f);
+        }
+    };
+    for (int s = wave; s < slabs; s += kAtOnce * waves) some(s, (s + (kAtOnce - 1) * waves + 1) * kSlab <= p.kbytes);
+    part[wave * 64 + lane] = acc;
+    __syncthreads();
+    const float* bias = p.bias ? p.bias + (GROUPED ? (int64_t)e * p.N : 0) : nullptr;
+    for (int i = threadIdx.x; i < 256; i += blockDim.x) {
+        // (value i: row i / 16 of the tile, column i % 16: sum i % 4 of lane 16 (i / 4 % 4) + row)
+        const int r = i >> 4, n = n0 + (i & 15);
+        if (r >= rows || n >= p.N) continue;
+        const int from = (((i >> 2) & 3) * 16 + r) * 4 + (i & 3);
+        float s = 0.0f;
+        for (int k = 0; k < waves; ++k) s += reinterpret_cast<const float*>(part)[k * 256 + from];
+        if constexpr (GROUPED)
+            if (p.index && (uint32_t)p.index[m0 + r] >= (uint32_t)p.a_rows) s = 0.0f;
+        if (bias) s += bias[n];
+        static_cast<Elem<YT>*>(p.y)[(m0 + r) * p.y_row + n] = (Elem<YT>)act_of(s, p.act);
     }
 }
 
