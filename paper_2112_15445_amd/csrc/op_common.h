@@ -60,8 +60,11 @@ template <int ET> __device__ __forceinline__ v4i load_raw(const Elem<ET>* x)
 template <int ET> __device__ __forceinline__ v4i load_raw_part(const Elem<ET>* x, int have)
 {
     Elem<ET> e[kVec<ET>];
+    if (have <= 0) return v4i{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kVec<ET>; ++i) e[i] = i < have ? x[i] : (Elem<ET>)0.0f;
+    for (int i = 0; i < kVec<ET>; ++i) e[i] = x[min(i, have - 1)];       // (no branch a value: the loads go out together)
+#pragma unroll
+    for (int i = 0; i < kVec<ET>; ++i) e[i] = i < have ? e[i] : (Elem<ET>)0.0f;
     v4i raw;
     __builtin_memcpy(&raw, e, 16);
     return raw;
@@ -95,6 +98,34 @@ template <int V> __device__ __forceinline__ void store_codes(uint8_t* q, const f
     for (int i = 0; i < V / 4; ++i) w[i] = codes4(f[4 * i] * up, f[4 * i + 1] * up, f[4 * i + 2] * up, f[4 * i + 3] * up);
     if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(q) = w[0];
+}
+
+// Sums and maxima over the sixteen lanes of a row: four rotations within the row, which the vector unit does by itself (a shuffle
+// through LDS takes some 60 cycles each).
+template <int N> __device__ __forceinline__ float row_ror(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float sum16(float v)
+{
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    return v + row_ror<1>(v);
+}
+__device__ __forceinline__ float max16(float v)
+{
+    v = fmaxf(v, row_ror<8>(v));
+    v = fmaxf(v, row_ror<4>(v));
+    v = fmaxf(v, row_ror<2>(v));
+    return fmaxf(v, row_ror<1>(v));
+}
+// ... over the L = 16 or 32 lanes that hold 128 values.
+template <int L> __device__ __forceinline__ float max_block(float v)
+{
+    v = max16(v);
+    if constexpr (L == 32) v = fmaxf(v, __shfl_xor(v, 16));
+    return v;
 }
 
 inline sc_status_t launched() { return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP; }

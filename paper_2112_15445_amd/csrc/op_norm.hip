@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256;                // of a workgroup of the two-launch form
 constexpr int kMaxStretches = 64;            // stretches of positions of a sample
+constexpr int kParts = 1024;                 // statistics that a workgroup of the second launch takes in at a time
 
 struct NormArgs {
     const void* x;
@@ -32,21 +33,26 @@ struct NormArgs {
     int64_t x_sample, x_row, y_sample, y_row, s_row;
 };
 
-// Two sets of values as one: (n, mean, m2) takes in (n2, mean2, m2_2).
-__device__ __forceinline__ void join(float& n, float& mean, float& m2, float n2, float mean2, float m2_2)
-{
-    const float all = n + n2, d = mean2 - mean, share = all > 0.0f ? n2 / all : 0.0f;
-    mean += d * share;
-    m2 += m2_2 + d * d * n * share;
-    n = all;
-}
-
-// y of V neighbouring channels of one position.
-template <int ACT, int V>
-__device__ __forceinline__ void finish(float* f, const float* mean, const float* inv, const float* gam, const float* bet, int have)
+// V parameters from channel c on (the first `have`; `otherwise` where there are none).
+template <int V> __device__ __forceinline__ void load_params(float* out, const float* p, int c, int have, float otherwise)
 {
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = i < have ? activate<ACT>((f[i] - mean[i]) * inv[i] * gam[i] + bet[i]) : 0.0f;
+    for (int i = 0; i < V; ++i) out[i] = otherwise;
+    if (!p || have <= 0) return;
+    if (have >= V) {
+        __builtin_memcpy(out, p + c, 4 * V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = p[c + min(i, have - 1)];
+    }
+}
+
+// y of V neighbouring channels of one position; gam: gamma over the spread.
+template <int ACT, int V>
+__device__ __forceinline__ void finish(float* f, const float* mean, const float* gam, const float* bet, int have)
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = i < have ? activate<ACT>((f[i] - mean[i]) * gam[i] + bet[i]) : 0.0f;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -54,24 +60,27 @@ __device__ __forceinline__ void finish(float* f, const float* mean, const float*
 // others of the T lanes the positions; U positions a lane.  A sum over a group is a sum over lanes of a wave by shuffles and one over
 // the waves through LDS.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T) void norm_resident_kernel(NormArgs a, int TPR, int LPG)
+template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T, 4) void norm_resident_kernel(NormArgs a, int TPR, int LPG, int dies)
 {
     constexpr int V = kVec<XT>, W = T / 64;
     __shared__ float red[2][W][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int slabs = a.C / (TPR * V), n = blockIdx.x / slabs, c0 = (blockIdx.x - n * slabs) * TPR * V;
+    // dies: the workgroups of a sample go to one die, one after another, so that the pieces of a line that they read and write meet
+    // in its cache (workgroups are dealt to the eight dies in turn).
+    const int slabs = a.C / (TPR * V), of = dies ? blockIdx.x >> 3 : blockIdx.x, part = of / slabs;
+    const int n = dies ? part * 8 + (blockIdx.x & 7) : part, c0 = (of - part * slabs) * TPR * V;
+    if (n >= a.N) return;
     const int col = threadIdx.x & (TPR - 1), r0 = threadIdx.x / TPR, R = T / TPR, c = c0 + col * V;
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
-    float gam[V], bet[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        gam[i] = a.gamma ? a.gamma[c + i] : 1.0f;
-        bet[i] = a.beta ? a.beta[c + i] : 0.0f;
-    }
     v4i raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+        raw[u] = v4i{0, 0, 0, 0};
         if (r0 + u * R < a.S) raw[u] = load_raw<XT>(x + (r0 + u * R) * a.x_row);
+    }
+    float gam[V], bet[V];
+    load_params<V>(gam, a.gamma, c, V, 1.0f);
+    load_params<V>(bet, a.beta, c, V, 0.0f);
     const float cnt = (float)a.S * (float)a.Cg;
     auto total = [&](float v, int which) {
         for (int o = 1; o < LPG; o <<= 1) v += __shfl_xor(v, o);
@@ -95,6 +104,12 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T)
         }
     const float mean = total(s, 0) / cnt;
     s = 0.0f;
+    // (the values are widened again for each pass: kept wide, two-byte types would not fit the registers)
+    auto forget = [&] {
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(raw[u]));
+    };
+    forget();
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (r0 + u * R < a.S) {
@@ -105,29 +120,30 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T)
             s += part;
         }
     const float inv = 1.0f / sqrtf(total(s, 1) / cnt + a.eps);
-    float means[V], invs[V];
+    forget();
+    float means[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) means[i] = mean, invs[i] = inv;
+    for (int i = 0; i < V; ++i) means[i] = mean, gam[i] *= inv;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int pos = r0 + u * R;
         if (pos >= a.S) continue;            // (a position's lanes go on or leave together: the shuffles below stay inside it)
         float f[V];
         to_floats<XT>(raw[u], f);
-        finish<ACT, V>(f, means, invs, gam, bet, V);
+        finish<ACT, V>(f, means, gam, bet, V);
         Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c;
         if constexpr (YT == SC_ELEM_E4M3) {
             constexpr int L = kQBlock / V;
             float amax = kAmaxFloor;
 #pragma unroll
             for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
-#pragma unroll
-            for (int o = L / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+            amax = max_block<L>(amax);
             store_codes<V>(y, f, kCodeMax / amax);
             if (col % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + c / kQBlock] = amax / kCodeMax;
         } else {
             store_vec<YT, V>(y, f, V);
         }
+        if constexpr (U > 4) __builtin_amdgcn_sched_barrier(0);      // (one position at a time: sixteen under way do not fit the registers)
     }
 }
 
@@ -153,34 +169,41 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
     const int have = min(V, cn - v * V);
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + p0 * a.x_row + c0 + v * V;
     float mean[V] = {}, m2[V] = {}, cnt = 0.0f;
+    // (A batch is U positions, the last one as many as there are; the loads of a batch are under way while the one before is added up.)
+    auto load = [&](v4i* raw, int p) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            raw[u] = v4i{0, 0, 0, 0};
+            if (p + u * R < pn) raw[u] = have == V ? load_raw<XT>(x + (p + u * R) * a.x_row) : load_raw_part<XT>(x + (p + u * R) * a.x_row, have);
+        }
+    };
     if (r < R) {
-        int p = r;
-        for (; p + (U - 1) * R < pn; p += U * R) {
-            v4i raw[U];
-            if (have == V) {
+        v4i raw[U];
+        load(raw, r);
+        for (int p = r; p < pn; p += U * R) {
+            v4i now[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = load_raw<XT>(x + (p + u * R) * a.x_row);
-            } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = load_raw_part<XT>(x + (p + u * R) * a.x_row, have);
-            }
-            const float share = (float)U / (cnt + (float)U);
+            for (int u = 0; u < U; ++u) now[u] = raw[u];
+            if (p + U * R < pn) load(raw, p + U * R);
+            const int valid = min(U, (pn - p + R - 1) / R);
+            const float n2 = (float)valid, share = n2 / (cnt + n2), each = 1.0f / n2;
             float sum[V] = {}, sq[V] = {};
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float f[V];
-                to_floats<XT>(raw[u], f);
+                to_floats<XT>(now[u], f);
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[i] += f[i];
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] *= 1.0f / U;
+            for (int i = 0; i < V; ++i) sum[i] *= each;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float f[V];
-                to_floats<XT>(raw[u], f);
+                to_floats<XT>(now[u], f);
+                if (u < valid)
 #pragma unroll
-                for (int i = 0; i < V; ++i) sq[i] += (f[i] - sum[i]) * (f[i] - sum[i]);
+                    for (int i = 0; i < V; ++i) sq[i] += (f[i] - sum[i]) * (f[i] - sum[i]);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -188,19 +211,7 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
                 mean[i] += d * share;
                 m2[i] += sq[i] + d * d * cnt * share;
             }
-            cnt += (float)U;
-        }
-        for (; p < pn; p += R) {
-            float f[V];
-            to_floats<XT>(have == V ? load_raw<XT>(x + p * a.x_row) : load_raw_part<XT>(x + p * a.x_row, have), f);
-            cnt += 1.0f;
-            const float share = 1.0f / cnt;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = f[i] - mean[i];
-                mean[i] += d * share;
-                m2[i] += d * (f[i] - mean[i]);
-            }
+            cnt += n2;
         }
     }
 #pragma unroll
@@ -220,15 +231,14 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
             const int rr = i / gc, cc = g * gc + (i - rr * gc);
             s += ns[rr * tpr + cc / V] * ms[rr * tpr * V + cc];
         }
-        for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o);
-        const float m = s / total;
+        const float m = sum16(s) / total;
         float q = 0.0f;
         for (int i = sl; i < R * gc; i += 16) {
             const int rr = i / gc, cc = g * gc + (i - rr * gc);
             const float d = ms[rr * tpr * V + cc] - m;
             q += qs[rr * tpr * V + cc] + ns[rr * tpr + cc / V] * d * d;
         }
-        for (int o = 8; o; o >>= 1) q += __shfl_xor(q, o);
+        q = sum16(q);
         if (sl == 0) a.stats[(((int64_t)n * a.G + g0 + g) * a.stretches + st) * a.parts + part] = make_float2(m, q);
     }
 }
@@ -245,72 +255,95 @@ template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void n
     id /= wides;
     const int ch = id % chunks, n = id / chunks;
     const int c0 = sg * wide, cn = min(wide, a.C - c0);
-    const int g0 = c0 / a.Cg, groups = (c0 + cn - 1) / a.Cg - g0 + 1;
-    const int sub = threadIdx.x >> 4, sl = threadIdx.x & 15, per = a.stretches * a.parts;
-    for (int g = sub; g < groups; g += kThreads / 16) {
-        float cnt = 0.0f, mean = 0.0f, m2 = 0.0f;
-        const float2* st = a.stats + ((int64_t)n * a.G + g0 + g) * per;
-        for (int i = sl; i < per; i += 16) {
-            const int s = i / a.parts, part = i - s * a.parts;
-            const int chans = a.parts > 1 ? min(a.seg, a.Cg - part * a.seg) : a.Cg;
-            const float2 v = st[i];
-            join(cnt, mean, m2, (float)min(a.len, a.S - s * a.len) * (float)chans, v.x, v.y);
-        }
-        for (int o = 8; o; o >>= 1) {
-            const float n2 = __shfl_xor(cnt, o), mean2 = __shfl_xor(mean, o), q2 = __shfl_xor(m2, o);
-            if (sl & o) {                    // (both lanes of a pair join in the same order)
-                float n1 = n2, me = mean2, q = q2;
-                join(n1, me, q, cnt, mean, m2);
-                cnt = n1, mean = me, m2 = q;
-            } else {
-                join(cnt, mean, m2, n2, mean2, q2);
-            }
-        }
-        if (sl == 0) gs[g] = make_float2(mean, 1.0f / sqrtf(m2 / cnt + a.eps));
-    }
-    __syncthreads();
     const int tpr = CODES ? (cn + kQBlock - 1) / kQBlock * L : (cn + V - 1) / V;
     const int R = kThreads / tpr, r = threadIdx.x / tpr, v = threadIdx.x - r * tpr;
     const int have = min(V, cn - v * V), c = c0 + v * V;
-    float mean[V], inv[V], gam[V], bet[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        mean[i] = bet[i] = 0.0f, inv[i] = gam[i] = 1.0f;
-        if (i < have) {
-            const float2 s = gs[(c + i) / a.Cg - g0];
-            mean[i] = s.x, inv[i] = s.y;
-            if (a.gamma) gam[i] = a.gamma[c + i];
-            if (a.beta) bet[i] = a.beta[c + i];
-        }
-    }
-    if (r >= R) return;
-    const int p0 = ch * a.rows, p1 = min(a.S, p0 + a.rows);
+    const int p0 = ch * a.rows, p1 = r < R ? min(a.S, p0 + a.rows) : 0;
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
     Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + c;
-    for (int p = p0 + r; p < p1; p += U * R) {
-        v4i raw[U];
+    v4i raw[U];
+    auto load = [&](int p) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             raw[u] = v4i{0, 0, 0, 0};
-            if (p + u * R < p1) raw[u] = have == V ? load_raw<XT>(x + (p + u * R) * a.x_row) : load_raw_part<XT>(x + (p + u * R) * a.x_row, have);
+            if (p + u * R < p1 && have > 0) raw[u] = have == V ? load_raw<XT>(x + (p + u * R) * a.x_row) : load_raw_part<XT>(x + (p + u * R) * a.x_row, have);
+        }
+    };
+    // (what does not depend on the statistics is on its way while they are put together)
+    load(p0 + r);
+    float gam[V], bet[V];
+    load_params<V>(gam, a.gamma, c, have, 1.0f);
+    load_params<V>(bet, a.beta, c, have, 0.0f);
+    const int g0 = c0 / a.Cg, groups = (c0 + cn - 1) / a.Cg - g0 + 1;
+    // The stretches of as many groups as fit, all of them asked for at once (they come from the other dies' caches, 1-2 us away),
+    // then sixteen lanes a group.
+    __shared__ float2 parts_[kParts];
+    const int sub = threadIdx.x >> 4, sl = threadIdx.x & 15, per = a.stretches * a.parts, at_once = kParts / per;
+    const float total = (float)a.S * (float)a.Cg;
+    for (int gb = 0; gb < groups; gb += at_once) {
+        const int gn = min(at_once, groups - gb);
+        const float2* st = a.stats + ((int64_t)n * a.G + g0 + gb) * per;
+        float2 got[kParts / kThreads];
+#pragma unroll
+        for (int k = 0; k < kParts / kThreads; ++k)
+            if ((int)threadIdx.x + k * kThreads < gn * per) got[k] = st[threadIdx.x + k * kThreads];
+        if (gb) __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kParts / kThreads; ++k)
+            if ((int)threadIdx.x + k * kThreads < gn * per) parts_[threadIdx.x + k * kThreads] = got[k];
+        __syncthreads();
+        for (int g = sub; g < gn; g += kThreads / 16) {
+            auto count = [&](int i) {
+                const int st_ = a.parts > 1 ? i / a.parts : i, part = i - st_ * a.parts;
+                return (float)min(a.len, a.S - st_ * a.len) * (float)(a.parts > 1 ? min(a.seg, a.Cg - part * a.seg) : a.Cg);
+            };
+            float mean = 0.0f, m2 = 0.0f;
+            for (int i = sl; i < per; i += 16) mean += count(i) * parts_[g * per + i].x;
+            mean = sum16(mean) / total;
+            for (int i = sl; i < per; i += 16) {
+                const float2 q = parts_[g * per + i];
+                m2 += q.y + count(i) * (q.x - mean) * (q.x - mean);
+            }
+            m2 = sum16(m2);
+            if (sl == 0) gs[gb + g] = make_float2(mean, 1.0f / sqrtf(m2 / total + a.eps));
+        }
+    }
+    __syncthreads();
+    float mean[V];
+    const int first = min(c, a.C - 1) / a.Cg;
+    int g = first, left = (first + 1) * a.Cg - c;            // (the group of a channel, and how many of its channels are to come)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 s = gs[min(g - g0, groups - 1)];
+        mean[i] = s.x, gam[i] *= s.y;
+        if (--left == 0) ++g, left = a.Cg;
+    }
+    for (int p = p0 + r; p < p1; p += U * R) {
+        v4i now[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) now[u] = raw[u];
+        if (p + U * R < p1) load(p + U * R);
+        float f[U][V], amax[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            to_floats<XT>(now[u], f[u]);
+            finish<ACT, V>(f[u], mean, gam, bet, have);
+            if constexpr (CODES) {
+                amax[u] = kAmaxFloor;
+#pragma unroll
+                for (int i = 0; i < V; ++i) amax[u] = fmaxf(amax[u], fabsf(f[u][i]));
+                amax[u] = max_block<L>(amax[u]);         // (a block's lanes have the same position: all of it counts or none)
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int pos = p + u * R;
-            if (pos >= p1) break;            // (the lanes of a position leave together)
-            float f[V];
-            to_floats<XT>(raw[u], f);
-            finish<ACT, V>(f, mean, inv, gam, bet, have);
+            if (pos >= p1) break;
             if constexpr (CODES) {
-                float amax = kAmaxFloor;
-#pragma unroll
-                for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
-#pragma unroll
-                for (int o = L / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-                if (c < ((a.C + 15) & ~15)) store_codes<V>(y + pos * a.y_row, f, kCodeMax / amax);
-                if (v % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + c / kQBlock] = amax / kCodeMax;
+                if (c < ((a.C + 15) & ~15)) store_codes<V>(y + pos * a.y_row, f[u], kCodeMax / amax[u]);
+                if (v % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + c / kQBlock] = amax[u] / kCodeMax;
             } else {
-                store_vec<YT, V>(y + pos * a.y_row, f, have);
+                store_vec<YT, V>(y + pos * a.y_row, f[u], have);
             }
         }
     }
@@ -319,28 +352,31 @@ template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void n
 bool pow2(int v) { return v > 0 && (v & (v - 1)) == 0; }
 
 struct NormShape {
-    int TPR, LPG, T, U;                      // one launch (TPR = 0: two)
+    int TPR, LPG, T, U, dies;                // one launch (TPR = 0: two)
     int seg, segs, parts, len, stretches;    // the statistics
     int wide, wides, rows, chunks;           // the result
     size_t bytes;
 };
 
-// One launch: groups of a power of two of 16-byte lanes, channels of a workgroup whole 128-byte lines (codes: whole blocks) where
-// C allows it, and all positions of them in 16 vectors a lane of 512.
+// One launch: groups of a power of two of 16-byte lanes, all positions of a workgroup's channels in 16 vectors a lane of 1024.  The
+// channels of a workgroup make whole 128-byte lines where that fits, else the most that fits, down to 32 bytes (codes: whole
+// blocks of 128 channels always).
 bool norm_resident(const sc_group_norm_t* d, NormShape* s)
 {
-    const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G;
+    const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G, most = 1024 * 16;
+    const bool codes = d->y_type == SC_ELEM_E4M3;
     if (Cg % V || !pow2(Cg / V) || Cg / V > 64) return false;
-    const int LPG = Cg / V, line = d->y_type == SC_ELEM_E4M3 ? kQBlock / V : 8;
+    const int LPG = Cg / V, line = codes ? kQBlock / V : 8;
     int TPR = LPG;
-    while (TPR < line && d->C % (2 * TPR * V) == 0) TPR *= 2;
-    if (TPR > 64 || (d->y_type == SC_ELEM_E4M3 && TPR % line)) return false;
+    while (TPR < line && d->C % (2 * TPR * V) == 0 && (codes || TPR < 2 || (int64_t)d->S * TPR * 2 <= most)) TPR *= 2;
+    if (TPR > 64 || (codes && TPR % line) || (TPR < 2 && d->C != TPR * V)) return false;
     const int64_t vectors = (int64_t)d->S * TPR;
-    if (vectors > 512 * 16) return false;
+    if (vectors > most) return false;
     s->TPR = TPR;
     s->LPG = LPG;
-    s->T = vectors <= 256 * 4 ? 256 : 512;
+    s->T = vectors <= 256 * 4 ? 256 : vectors <= 512 * 16 ? 512 : 1024;
     s->U = vectors <= s->T * 4 ? 4 : 16;
+    s->dies = d->N >= 16 || d->N == 8;
     return true;
 }
 
@@ -361,7 +397,7 @@ NormShape norm_shape(const sc_group_norm_t* d)
     // Four workgroups a compute unit for both launches, no stretch under eight vectors a lane.
     const int R = std::max<int>(1, kThreads / (int)ceil_div(std::min(s.seg, d->C), V));
     const int64_t want = std::max<int64_t>(1, 1024 / ((int64_t)d->N * s.segs));
-    s.stretches = (int)std::min<int64_t>({want, kMaxStretches, ceil_div(d->S, 8 * R)});
+    s.stretches = (int)std::min<int64_t>({want, kMaxStretches, kParts / s.parts, ceil_div(d->S, 8 * R)});
     s.len = (int)ceil_div(d->S, s.stretches);
     s.stretches = (int)ceil_div(d->S, s.len);
     s.wide = std::min(most, d->C);
@@ -381,6 +417,7 @@ sc_status_t check_norm(const sc_group_norm_t* d)
     if (!is_wide(d->x_type) || (d->y_type != d->x_type && d->y_type != SC_ELEM_E4M3)) return SC_ERR_UNSUPPORTED;
     if (d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || !(d->eps >= 0.0f) || d->eps > 3e38f) return SC_ERR_UNSUPPORTED;
     if ((int64_t)d->S * d->C >= (int64_t)1 << 31 || (int64_t)d->N * d->S >= (int64_t)1 << 31) return SC_ERR_RANGE;
+    if (d->C / d->G >= 1 << 20) return SC_ERR_RANGE;         // (the parts of a group: kParts of 1024 channels or more)
     if (d->x_sample < 0 || d->x_row < 0) return SC_ERR_SHAPE;
     if (d->y_row < d->C) return SC_ERR_SHAPE;
     if (d->N > 1 && d->S > 0 && d->y_sample < (d->S - 1) * d->y_row + d->C) return SC_ERR_SHAPE;
@@ -394,12 +431,13 @@ sc_status_t check_norm(const sc_group_norm_t* d)
 template <int XT, int YT, int ACT> sc_status_t launch_norm(const sc_group_norm_t* d, const NormShape& s, const NormArgs& a, hipStream_t stream)
 {
     if (s.TPR) {
-        const int64_t blocks = (int64_t)d->N * (d->C / (s.TPR * kVec<XT>));
+        const int64_t blocks = (s.dies ? ceil_div(d->N, 8) * 8 : (int64_t)d->N) * (d->C / (s.TPR * kVec<XT>));
         if (blocks * s.T >= (int64_t)1 << 32) return SC_ERR_RANGE;
         const dim3 grid((unsigned)blocks);
-        if (s.T == 256) norm_resident_kernel<XT, YT, ACT, 256, 4><<<grid, 256, 0, stream>>>(a, s.TPR, s.LPG);
-        else if (s.U == 4) norm_resident_kernel<XT, YT, ACT, 512, 4><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG);
-        else norm_resident_kernel<XT, YT, ACT, 512, 16><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG);
+        if (s.T == 256) norm_resident_kernel<XT, YT, ACT, 256, 4><<<grid, 256, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
+        else if (s.U == 4) norm_resident_kernel<XT, YT, ACT, 512, 4><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
+        else if (s.T == 512) norm_resident_kernel<XT, YT, ACT, 512, 16><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
+        else norm_resident_kernel<XT, YT, ACT, 1024, 16><<<grid, 1024, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
         return launched();
     }
     const int64_t first = (int64_t)d->N * s.segs * s.stretches, second = (int64_t)d->N * s.wides * s.chunks;

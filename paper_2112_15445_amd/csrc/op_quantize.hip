@@ -37,8 +37,7 @@ template <int XT> __global__ __launch_bounds__(256) void quantize_rows_kernel(Qu
         to_floats<XT>(raw[u], f);
 #pragma unroll
         for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
-#pragma unroll
-        for (int o = L / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+        amax = max_block<L>(amax);
         if (first + u * (256 / L) >= items) continue;
         if (col[u] < ((a.K + 15) & ~15)) store_codes<V>(a.q + row[u] * a.q_row + col[u], f, kCodeMax / amax);
         if (part == 0) a.scale[row[u] * a.s_row + col[u] / kQBlock] = amax / kCodeMax;
