@@ -96,6 +96,18 @@ template <int ET, int V> __device__ __forceinline__ void store_vec(Elem<ET>* y, 
             if (i < have) y[i] = v[i];
     }
 }
+// The same past the caches, for y on 16 bytes and whole.
+template <int ET, int V> __device__ __forceinline__ void store_vec_past(Elem<ET>* y, const float* f)
+{
+    typedef Elem<ET> vec __attribute__((ext_vector_type(V)));
+    vec v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (Elem<ET>)f[i];
+    struct raw { v4i q[V * sizeof(Elem<ET>) / 16]; } r;
+    __builtin_memcpy(&r, &v, sizeof(r));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(r) / 16; ++i) __builtin_nontemporal_store(r.q[i], reinterpret_cast<v4i*>(y) + i);
+}
 // The V codes of f * up; q on V bytes (zeros of f behind the end of a row become zero codes).
 template <int V> __device__ __forceinline__ void store_codes(uint8_t* q, const float* f, float up)
 {

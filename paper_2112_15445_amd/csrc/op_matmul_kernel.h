@@ -78,46 +78,52 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int e, int M,
     hi = max(lo, min(max(offsets[e + 1], 0), M));
 }
 
-// Group and rows of row tile `tile` (of BT rows) of all groups: every wave adds up the groups' tiles, 64 groups at a time.
-// *total = row tiles in all, known where the tile is none of them (e = -1) and never smaller than tile + 1 else.
-template <int BT> __device__ __forceinline__ int group_tile_count(const MatmulArgs& p)
-{
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int base = 0; base < p.E; base += 64) {
-        int lo = 0, hi = 0;
-        if (base + lane < p.E) group_rows(p.offsets, base + lane, p.M, lo, hi);
-        int t = (hi - lo + BT - 1) / BT;
-        for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
-        total += t;
-    }
-    return __builtin_amdgcn_readfirstlane(total);
-}
+// The row tiles (of BT rows) of the groups, 64 groups a turn: every wave adds them up for itself.  Up to 64 groups are read once.
+template <int BT> struct GroupTiles {
+    int lo, hi, upto;                        // this lane's group of the turn: its rows, row tiles of the groups up to it
+    int base = 0, before = 0, total = 0;     // first group of the turn, row tiles of the turns before, of all
 
-template <int BT> __device__ __forceinline__ bool find_group(const MatmulArgs& p, int tile, int& e, int& m0, int& hi_)
-{
-    const int lane = threadIdx.x & 63;
-    for (int base = 0; base < p.E; base += 64) {
-        int lo = 0, hi = 0;
-        if (base + lane < p.E) group_rows(p.offsets, base + lane, p.M, lo, hi);
-        const int t = (hi - lo + BT - 1) / BT;
-        int upto = t;                                            // tiles of the groups up to this lane's
+    // tiles of the 64 groups from `first` on
+    __device__ __forceinline__ int turn(const MatmulArgs& p, int first)
+    {
+        const int lane = threadIdx.x & 63;
+        lo = hi = 0;
+        if (first + lane < p.E) group_rows(p.offsets, first + lane, p.M, lo, hi);
+        upto = (hi - lo + BT - 1) / BT;
         for (int o = 1; o < 64; o <<= 1) {
             const int v = __shfl_up(upto, o);
             if (lane >= o) upto += v;
         }
-        const uint64_t behind = __ballot(tile < upto);
-        if (behind) {
-            const int at = __builtin_ctzll(behind);
-            e = __builtin_amdgcn_readfirstlane(base + at);
-            m0 = __builtin_amdgcn_readfirstlane(__shfl(lo + (tile - (upto - t)) * BT, at));
-            hi_ = __builtin_amdgcn_readfirstlane(__shfl(hi, at));
-            return true;
-        }
-        tile -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        return __builtin_amdgcn_readlane(upto, 63);
     }
-    return false;
-}
+    __device__ __forceinline__ explicit GroupTiles(const MatmulArgs& p)
+    {
+        total = turn(p, 0);
+        if (p.E > 64) {
+            for (int f = 64; f < p.E; f += 64) total += turn(p, f);
+            base = -1;                       // (the turn in the registers is the last one)
+        }
+    }
+    // Group e of row tile `tile` < total, its first row and the end of its group.
+    __device__ __forceinline__ void find(const MatmulArgs& p, int tile, int& e, int& m0, int& end)
+    {
+        if (base < 0)
+            for (base = 0, before = 0;; base += 64) {
+                const int t = turn(p, base);
+                if (tile < before + t) break;
+                before += t;
+            }
+        const int at = __builtin_ctzll(__ballot(tile - before < upto));
+        const int l = __builtin_amdgcn_readlane(lo, at), h = __builtin_amdgcn_readlane(hi, at), u = __builtin_amdgcn_readlane(upto, at);
+        e = base + at;
+        m0 = l + (tile - before - (u - (h - l + BT - 1) / BT)) * BT;
+        end = h;
+    }
+};
+
+struct NoGroups {
+    __device__ __forceinline__ explicit NoGroups(const MatmulArgs&) {}
+};
 
 // One 16-byte (or 4-byte) direct-to-LDS load a lane: lane i's bytes go to `lds` + i * width.  Written by hand so that the compiler does
 // not make the reads of the other buffer wait for it; the caller waits on vmcnt itself (staged()), which is also what keeps reads of
@@ -167,6 +173,13 @@ template <int YT> __device__ __forceinline__ v4f block_product(const v4i* x, con
     return d;
 }
 
+// sums + the product of 16 weight rows (x) and 16 rows of a (z), 32 values of 16 bits of each.
+template <int AT> __device__ __forceinline__ v4f product16(v4i x, v4i z, v4f sums)
+{
+    if constexpr (AT == SC_ELEM_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, z), sums, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, x), __builtin_bit_cast(v8b, z), sums, 0, 0, 0);
+}
+
 // acc += one slab's product of 16 weight rows (x) and 16 rows of a (z); codes: times the scale of the block.
 template <int AT, int YT> __device__ __forceinline__ void multiply(v4f& acc, const v4i* x, const v4i* z, float scale)
 {
@@ -177,9 +190,7 @@ template <int AT, int YT> __device__ __forceinline__ void multiply(v4f& acc, con
     } else {
         (void)scale;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if constexpr (AT == SC_ELEM_F16) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x[h]), __builtin_bit_cast(v8h, z[h]), acc, 0, 0, 0);
-            else acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, x[h]), __builtin_bit_cast(v8b, z[h]), acc, 0, 0, 0);
+        for (int h = 0; h < 2; ++h) acc = product16<AT>(x[h], z[h], acc);
     }
 }
 
@@ -209,7 +220,9 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
 
     // The place of this workgroup: neighbours in the order of launch go to different XCDs, so the ids are dealt out again such
     // that an XCD walks over neighbouring tiles, eight row tiles by eight column tiles at a time.
-    int ntm = GROUPED ? group_tile_count<BT>(p) : (p.M + BT - 1) / BT;
+    int ntm = (p.M + BT - 1) / BT;
+    std::conditional_t<GROUPED, GroupTiles<BT>, NoGroups> groups(p);
+    if constexpr (GROUPED) ntm = groups.total;
     const int total = ntm * ntn;
     int id = blockIdx.x;
     if (id >= total) return;
@@ -221,8 +234,7 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
     // (divisions are done in vector registers; what comes of these is the same in every lane and belongs in scalar ones)
     const int tn = __builtin_amdgcn_readfirstlane(inband / height), tm = __builtin_amdgcn_readfirstlane(band * 8 + inband - tn * height);
     int e = 0, m0 = tm * BT, hi = p.M;
-    if constexpr (GROUPED)
-        if (!find_group<BT>(p, tm, e, m0, hi)) return;
+    if constexpr (GROUPED) groups.find(p, tm, e, m0, hi);
     const int n0 = tn * BN;
     const int rows = min(BT, hi - m0);
 
@@ -365,14 +377,18 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             if (CODES && i == 1)
 #pragma unroll
                 for (int j = 0; j < TF; ++j) sc[j] *= sw;
+            if constexpr (CODES) {
 #pragma unroll
-            for (int j = 0; j < TF; ++j) {
-                if constexpr (CODES) {
+                for (int j = 0; j < TF; ++j) {
                     d[i & 1][j] = block_product<YT>(w[i % 3], t[j]);
                     if (i > 0) add(i - 1, j);
-                } else {
-                    multiply<AT, YT>(acc[i][j], w[i % 3], t[j], 0.0f);
                 }
+            } else {
+                // (the two halves of a slab's product add to the same sums: one half of all products, then the other)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < TF; ++j) acc[i][j] = product16<AT>(w[i % 3][h], t[j][h], acc[i][j]);
             }
             // In the widest tile: the reads first, then the scaling of one product under each matrix instruction (245 us against 252 at
             // 8192 x 8192 x 4096; narrower tiles lose by it).
@@ -434,7 +450,9 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             float z[8];
 #pragma unroll
             for (int v = 0; v < 8; ++v) z[v] = act_of((zero[j] ? 0.0f : acc[i + (v >> 2)][j][v & 3]) + add[v], p.act);
-            if (wide) {
+            if (wide && whole8) {
+                store_vec_past<YT, 8>(y, z);
+            } else if (wide) {
                 store_vec<YT, 8>(y, z, p.N - n);
             } else {
 #pragma unroll
@@ -456,8 +474,11 @@ template <int AT, int YT, bool GROUPED> __global__ __launch_bounds__(512) void m
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int ntn = (p.N + 15) / 16, tm = blockIdx.x / ntn, n0 = (blockIdx.x - tm * ntn) * 16;
     int e = 0, m0 = tm * 16, hi = p.M;
-    if constexpr (GROUPED)
-        if (!find_group<16>(p, tm, e, m0, hi)) return;
+    if constexpr (GROUPED) {
+        GroupTiles<16> groups(p);
+        if (tm >= groups.total) return;
+        groups.find(p, tm, e, m0, hi);
+    }
     const int rows = min(16, hi - m0), c = lane & 15, q = lane >> 4;
     const uint8_t* w = p.b + (GROUPED ? e * p.b_expert : 0) + min(n0 + c, p.N - 1) * p.b_row + q * 16;
     const float* bs = CODES ? p.bs + (GROUPED ? e * p.bs_expert : 0) + n0 / kQBlock * p.bs_row : nullptr;
