@@ -553,8 +553,9 @@ sc_status_t sparse_conv_matmul_blocks_workspace_size(const sc_matmul_blocks_t* d
 /*   a, b device codes, 16-byte aligned, every row readable up to the next multiple of 16 columns (what lies
  *        between column K and there is ignored)       bias [N] device f32 or NULL
  *   y    device, element-aligned
+ * The forms that there are take no workspace: the size is 0.
  * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (types, activation, alignment), SC_ERR_RANGE
- * (a row of codes of 2^22 bytes or more, a block of 256 rows of y of 2^31 bytes or more), SC_ERR_WORKSPACE, SC_ERR_HIP. */
+ * (a distance between rows of 2^22 bytes or more, M > 2^30, more workgroups than a launch has), SC_ERR_HIP. */
 sc_status_t sparse_conv_matmul_blocks(const sc_matmul_blocks_t* d, const void* a, const float* a_scale, const void* b,
                                       const float* b_scale, const float* bias, void* y, void* workspace_dev,
                                       size_t workspace_bytes, void* stream);

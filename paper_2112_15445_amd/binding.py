@@ -502,3 +502,98 @@ def forward_torch(plan: Plan, x, y=None, workspace=None):
                  workspace.data_ptr() if workspace is not None else 0,
                  workspace.numel() * workspace.element_size() if workspace is not None else 0, stream)
     return y
+
+
+# ... and of the operators of channels-last blocks: tensors in, tensors out, on torch's current stream.  Rows may lie further apart than
+# their length; the last dimension is contiguous.
+
+def _stream(t) -> int:
+    import torch
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _workspace(op, like):
+    import torch
+    n = op.workspace_size()
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
+
+
+def _ptr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _rows(t, what: str):
+    if not t.is_cuda or t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: a GPU tensor with a contiguous last dimension")
+    return t
+
+
+def _params(t, n: int, what: str):
+    import torch
+    if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
+        raise ValueError(f"{what}: {n} contiguous 32-bit floats on the GPU")
+    return t
+
+
+def empty_codes(*shape, device="cuda"):
+    """A tensor for codes, its rows on 16 bytes."""
+    import torch
+    return torch.empty(*shape[:-1], _up(shape[-1], 16), dtype=torch.float8_e4m3fn, device=device)[..., :shape[-1]]
+
+
+def group_norm_torch(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, act: str = "none", codes: bool = False):
+    """act(group norm) of x [N, S, C], channels last: a tensor like x, or with codes = True (e4m3 codes [N S, C], scales)."""
+    import torch
+    _rows(x, "x")
+    N, S, C = x.shape
+    y = empty_codes(N * S, C, device=x.device) if codes else torch.empty((N, S, C), dtype=x.dtype, device=x.device)
+    scale = torch.empty(N * S, -(-C // BLOCK), device=x.device) if codes else None
+    op = GroupNorm(N, S, C, groups, eps=eps, act=act, x_type=x.dtype, y_type=y.dtype, x_strides=x.stride()[:2])
+    ws, n = _workspace(op, x)
+    op.forward(x.data_ptr(), _ptr(_params(gamma, C, "gamma")), _ptr(_params(beta, C, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n, _stream(x))
+    return (y, scale) if codes else y
+
+
+def quantize_blocks_torch(x, rows: int = 1):
+    """(e4m3 codes, scales) of a matrix [M, K] in blocks of rows x 128; a stack [E, M, K] matrix by matrix."""
+    import torch
+    _rows(x, "x")
+    lead, (M, K) = x.shape[:-2], x.shape[-2:]
+    q = empty_codes(*lead, M, K, device=x.device)
+    scale = torch.empty(*lead, -(-M // rows), -(-K // BLOCK), device=x.device)
+    op = BlockQuantizer(M, K, rows=rows, x_type=x.dtype, x_row=x.stride(-2), q_row=q.stride(-2))
+    for i in np.ndindex(*lead):
+        op.forward(x[i].data_ptr(), q[i].data_ptr(), scale[i].data_ptr(), _stream(x))
+    return q, scale
+
+
+def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dtype=None):
+    """act(a b^T + bias) of codes a [M, K] with scales of 1 x 128 and b [N, K] with scales of 128 x 128 blocks."""
+    import torch
+    (M, K), N = _rows(a, "a").shape, _rows(b, "b").shape[0]
+    if b.shape[1] != K:
+        raise ValueError(f"b has {b.shape[1]} columns, a has {K}")
+    y = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=a.device)
+    op = BlockMatmul(M, N, K, y_type=y.dtype, act=act, a_row=a.stride(0), b_row=b.stride(0), a_scale_row=a_scale.stride(0), b_scale_row=b_scale.stride(0))
+    ws, n = _workspace(op, a)
+    op.forward(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(_params(bias, N, "bias")), y.data_ptr(), _ptr(ws), n, _stream(a))
+    return y
+
+
+def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, bias=None, act: str = "none", dtype=None):
+    """Rows offsets[e] .. offsets[e+1] - 1 of the result: act(a[index] b[e]^T + bias[e]); a [rows, K], b [E, N, K], f16, bf16 or
+    codes with their scales; offsets and index 32-bit integers on the GPU."""
+    import torch
+    _rows(a, "a"), _rows(b, "b")
+    E, N, K = b.shape
+    if a.shape[1] != K or a.dtype != b.dtype or offsets.dtype != torch.int32 or offsets.numel() != E + 1 or (index is not None and index.dtype != torch.int32):
+        raise ValueError("a [rows, K] and b [E, N, K] of one type, offsets [E + 1] and index in 32-bit integers")
+    M = a.shape[0] if index is None else index.numel()
+    codes = a.dtype == torch.float8_e4m3fn
+    y = torch.empty(M, N, dtype=dtype or (torch.bfloat16 if codes else a.dtype), device=a.device)
+    op = GroupedMatmul(M, N, K, E, a_type=a.dtype, y_type=y.dtype, act=act, a_rows=a.shape[0], a_row=a.stride(0), b_row=b.stride(1), b_expert=b.stride(0),
+                       a_scale_row=a_scale.stride(0) if codes else 0, b_scale_row=b_scale.stride(1) if codes else 0, b_scale_expert=b_scale.stride(0) if codes else 0)
+    ws, n = _workspace(op, a)
+    op.forward(a.data_ptr(), _ptr(a_scale), _ptr(index), offsets.contiguous().data_ptr(), b.data_ptr(), _ptr(b_scale), _ptr(_params(bias, E * N, "bias")),
+               y.data_ptr(), _ptr(ws), n, _stream(a))
+    return y

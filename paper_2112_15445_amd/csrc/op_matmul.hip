@@ -65,7 +65,8 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch(const MatmulArgs& p, 
     else return SC_ERR_UNSUPPORTED;
 }
 
-constexpr int64_t kMaxRowBytes = (int64_t)1 << 22;
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 22;     // (256 rows of a tile are addressed with 32 bits)
+constexpr int kMaxRows = 1 << 30;
 
 sc_status_t check_blocks(const sc_matmul_blocks_t* d)
 {
@@ -74,7 +75,7 @@ sc_status_t check_blocks(const sc_matmul_blocks_t* d)
     if (d->M < 0 || d->N <= 0 || d->K <= 0 || d->a_row < d->K || d->b_row < d->K || d->y_row < d->N || d->a_scale_row < KB || d->b_scale_row < KB)
         return SC_ERR_SHAPE;
     if (!is_wide(d->y_type) || d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || d->a_row % 16 || d->b_row % 16) return SC_ERR_UNSUPPORTED;
-    if (d->a_row >= kMaxRowBytes || d->b_row >= kMaxRowBytes || d->y_row * 4 * 256 >= (int64_t)1 << 31) return SC_ERR_RANGE;
+    if (d->M > kMaxRows || d->a_row >= kMaxRowBytes || d->b_row >= kMaxRowBytes) return SC_ERR_RANGE;
     return SC_OK;
 }
 
@@ -89,7 +90,7 @@ sc_status_t check_grouped(const sc_matmul_grouped_t* d)
     if (d->b_expert < (d->N - 1) * d->b_row + d->K && d->E > 1) return SC_ERR_SHAPE;
     if (codes && (d->a_scale_row < KB || d->b_scale_row < KB || (d->E > 1 && d->b_scale_expert < ceil_div(d->N, kQBlock) * KB))) return SC_ERR_SHAPE;
     if (d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || d->a_row * e % 16 || d->b_row * e % 16 || d->b_expert * e % 16) return SC_ERR_UNSUPPORTED;
-    if (d->a_row * e >= kMaxRowBytes || d->b_row * e >= kMaxRowBytes || d->y_row * 4 * 256 >= (int64_t)1 << 31) return SC_ERR_RANGE;
+    if (d->M > kMaxRows || d->a_row * e >= kMaxRowBytes || d->b_row * e >= kMaxRowBytes) return SC_ERR_RANGE;
     return SC_OK;
 }
 

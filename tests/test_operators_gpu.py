@@ -436,3 +436,114 @@ def test_matmul_grouped_with_offsets_that_are_out_of_range():
 def test_matmul_grouped_of_no_rows():
     B.GroupedMatmul(0, 16, 16, 2, a_type="f16").forward(0, 0, 0, 0, 0, 0, 0, 0, 0, 0, stream())
     torch.cuda.synchronize()
+
+
+# -- how they are called ---------------------------------------------------------------------------
+
+def test_torch_conveniences_and_the_example():
+    """The block of examples/channels_last_experts.py: norm to codes, router, grouped products, against the same in 32 bits.  Codes are off
+    by up to 2^-4 of a value (3 % rms), and two products follow one another: a few percent of what the block adds."""
+    import importlib.util
+    import os
+    spec = importlib.util.spec_from_file_location("example", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "channels_last_experts.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    assert m.main(2, 7, 9, 192) < 0.1
+    assert m.main(1, 1, 1, 64) < 0.1
+
+
+def test_torch_conveniences_refuse():
+    x = torch.zeros(2, 4, 32, device="cuda", dtype=torch.float16)
+    with pytest.raises(ValueError):
+        B.group_norm_torch(x.transpose(1, 2), 4)
+    with pytest.raises(ValueError):
+        B.group_norm_torch(x, 4, gamma=torch.ones(32, device="cuda", dtype=torch.float16))
+    with pytest.raises(ValueError):
+        B.quantize_blocks_torch(torch.zeros(4, 32))
+    q, s = B.quantize_blocks_torch(torch.zeros(4, 32, device="cuda"))
+    w, t = B.quantize_blocks_torch(torch.zeros(4, 48, device="cuda"), 128)
+    with pytest.raises(ValueError):
+        B.matmul_blocks_torch(q, s, w, t)
+    with pytest.raises(ValueError):
+        B.matmul_grouped_torch(x[0], x.bfloat16(), torch.zeros(3, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        B.matmul_grouped_torch(x[0], x, torch.zeros(3, dtype=torch.int64, device="cuda"))
+
+
+def _calls():
+    """One call of each operator (of each form of the group norm and the products) on its own buffers: (run, outputs)."""
+    rng = np.random.default_rng(11)
+    out = []
+    for N, S, C, G, y_type in ((2, 49, 256, 32, "f16"), (2, 3000, 48, 3, "f16"), (1, 500, 360, 30, "e4m3")):
+        x, gamma, beta = norm_inputs(N, S, C, 6)
+        xd, g, b = torch.from_numpy(x).cuda().half(), torch.from_numpy(gamma).cuda(), torch.from_numpy(beta).cuda()
+        y = B.empty_codes(N * S, C) if y_type == "e4m3" else torch.empty_like(xd)
+        ys = torch.empty(N * S, -(-C // 128), device="cuda")
+        op = B.GroupNorm(N, S, C, G, act="silu", x_type="f16", y_type=y_type)
+        ws, wp, wn = workspace(op)
+        keep = (xd, g, b, ws)
+        out.append((lambda st, op=op, y=y, ys=ys, wp=wp, wn=wn, k=keep: op.forward(k[0].data_ptr(), k[1].data_ptr(), k[2].data_ptr(), y.data_ptr(), ys.data_ptr(), wp, wn, st), y, xd))
+    x = torch.from_numpy(rng.normal(size=(200, 300)).astype(np.float32)).cuda()
+    for rows in (1, 128):
+        q, s = B.empty_codes(200, 300), torch.empty(-(-200 // rows), 3, device="cuda")
+        op = B.BlockQuantizer(200, 300, rows=rows, x_type="f32")
+        out.append((lambda st, op=op, q=q, s=s: op.forward(x.data_ptr(), q.data_ptr(), s.data_ptr(), st), q, x))
+    for M, N, K in ((3, 200, 600), (100, 600, 300), (1000, 2100, 300)):
+        a, sa = B.quantize_blocks_torch(torch.from_numpy(rng.normal(size=(M, K)).astype(np.float32)).cuda())
+        b, sb = B.quantize_blocks_torch(torch.from_numpy(rng.normal(size=(N, K)).astype(np.float32)).cuda(), 128)
+        y = torch.empty(M, N, device="cuda")
+        op = B.BlockMatmul(M, N, K, y_type="f32")
+        ws, wp, wn = workspace(op)
+        out.append((lambda st, op=op, y=y, k=(a, sa, b, sb, ws), wp=wp, wn=wn: op.forward(k[0].data_ptr(), k[1].data_ptr(), k[2].data_ptr(), k[3].data_ptr(), 0, y.data_ptr(), wp, wn, st), y, sa))
+    for counts in ([3, 0, 5], [100, 300, 2]):
+        off = torch.tensor(np.cumsum([0] + counts), dtype=torch.int32, device="cuda")
+        a, b = torch.randn(sum(counts), 256, device="cuda").half(), torch.randn(3, 1100, 256, device="cuda").half()
+        y = torch.empty(sum(counts), 1100, device="cuda", dtype=torch.float16)
+        op = B.GroupedMatmul(sum(counts), 1100, 256, 3, a_type="f16")
+        ws, wp, wn = workspace(op)
+        out.append((lambda st, op=op, y=y, k=(a, b, off, ws), wp=wp, wn=wn: op.forward(k[0].data_ptr(), 0, 0, k[2].data_ptr(), k[1].data_ptr(), 0, 0, y.data_ptr(), wp, wn, st), y, a))
+    return out
+
+
+def test_operators_on_another_stream_and_in_a_graph():
+    """Every call on a stream of its own after an input changed on it, then captured and replayed, inputs changing between the replays."""
+    s = torch.cuda.Stream()
+    for i, (run, y, x) in enumerate(_calls()):
+        print("case", i, tuple(y.shape), y.dtype, flush=True)
+        results = []
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for k in range(3):
+                x.mul_(2.0 if k == 1 else 1.0)
+                y.view(torch.uint8).zero_()
+                run(s.cuda_stream)
+                results.append(y.clone())
+        s.synchronize()
+        x.mul_(0.5)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            run(s.cuda_stream)
+        for k in range(3):
+            x.mul_(2.0 if k == 1 else 1.0)
+            y.view(torch.uint8).zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y.view(torch.uint8), results[k].view(torch.uint8)), (i, k)
+            torch.zeros(1000, device="cuda").sum().item()         # other work between the replays
+
+
+def test_rows_further_than_32_bits_reach():
+    """Activations and results whose last rows lie beyond 2^32 bytes."""
+    M, N, K, row = 1100, 96, 128, 1 << 22
+    a = torch.zeros(M, row - 16, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)      # 4.6 GB
+    q, s = B.quantize_blocks_torch(torch.randn(M, K, device="cuda"))
+    a[:, :K] = q
+    b, t = B.quantize_blocks_torch(torch.randn(N, K, device="cuda"), 128)
+    want = B.matmul_blocks_torch(q, s, b, t, dtype=torch.float32)
+    got = B.matmul_blocks_torch(a[:, :K], s, b, t, dtype=torch.float32)
+    assert torch.equal(got, want)
+    idx = torch.arange(M - 1, -1, -1, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    flipped = B.matmul_grouped_torch(a[:, :K], b[None], off, s, t[None], index=idx, dtype=torch.float32)
+    assert torch.equal(flipped, want.flip(0))

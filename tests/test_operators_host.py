@@ -105,7 +105,7 @@ def test_matmul_refusals():
     refused(UNSUPPORTED, M(1, 16, 32, a_row=40), *good)
     refused(UNSUPPORTED, M(1, 16, 32, b_row=33), *good)
     refused(RANGE, M(1, 16, 1 << 22), *good)
-    refused(RANGE, M(1, 1 << 21, 16), *good)
+    refused(RANGE, M((1 << 30) + 1, 16, 16), *good)
     for i in (0, 1, 2, 3, 5):
         refused(NULL, M(1, 16, 32), *[0 if j == i else v for j, v in enumerate(good)])
     for i, by in ((0, 8), (1, 2), (2, 4), (3, 1), (5, 1)):
