@@ -7,11 +7,11 @@
 namespace sc {
 namespace {
 
-template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN, int ST> sc_status_t launch_tile(const MatmulArgs& p, hipStream_t stream)
+template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN, int ST, int KS = 1> sc_status_t launch_tile(const MatmulArgs& p, hipStream_t stream)
 {
     const int64_t tiles = (ceil_div(p.M, BT) + (GROUPED ? std::min(p.E, p.M) : 0)) * ceil_div(p.N, BN);
-    if (tiles * WT * WN * 64 >= (int64_t)1 << 32) return SC_ERR_RANGE;
-    matmul_tile_kernel<AT, YT, GROUPED, BT, BN, WT, WN, ST><<<dim3((unsigned)tiles), WT * WN * 64, 0, stream>>>(p);
+    if (tiles * WT * WN * KS * 64 >= (int64_t)1 << 32) return SC_ERR_RANGE;
+    matmul_tile_kernel<AT, YT, GROUPED, BT, BN, WT, WN, ST, KS><<<dim3((unsigned)tiles), WT * WN * KS * 64, 0, stream>>>(p);
     return launched();
 }
 
@@ -26,27 +26,33 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch_rows(const MatmulArgs
 }
 
 // Which form.  Few rows: where its workgroups (16 x 16 of y) are at most two a compute unit (1 x 4096 x 4096: 7 us against 11 on
-// 64 x 64 tiles; 24 rows of that, three a unit: 11.8 against 11.5), and for products of up to 16 rows.  Else the tile whose estimate is smallest:
-// a fixed part, and per round of workgroups that are resident together a start and a time per slab, which is shorter in a last round
-// that leaves half of the places empty.  The constants, in microseconds, are fits to 259 products of 1 to 16384 rows, 4 to 64 groups,
-// 256 to 4096 columns and summed values, on which the choice costs 1.2 % more than the fastest of the forms each time.  (Groups: half a tile more each.)
-struct TileTime { int size, places; double start, slab, slab_half_empty; };
-constexpr TileTime kTiles[] = {{64, 512, 1.5, 0.52, 0.32}, {128, 512, 3.0, 1.2, 0.72}, {256, 256, 6.0, 1.85, 1.45}};
+// 64 x 64 tiles; 32 rows of that, four a unit: 11.6 against 11.6), and for products of up to 16 rows.  Else the tile whose estimate is
+// smallest: a fixed part, and per round of workgroups that are resident together a start and a time per slab, which is shorter in a last
+// round that leaves half of the places empty.  The constants, in microseconds, are fitted to 311 products of 1 to 16384 rows, 4 to 64
+// groups, 200 to 3200 columns and 256 to 4096 summed values in every pair of types; on these the choice costs 2.1 % more than the
+// fastest form each time, without the split 64 tile 3.2 %, without the 128 tile of eight waves 2.4 %.  (Groups: half a tile more each.)
+enum Form { kRows, kTile64, kTile64Split, kTile128, kTile128Deep, kTile256 };
+struct TileTime { Form form; int size, places; double start, slab, slab_half_empty; };
+constexpr TileTime kTiles[] = {{kTile64, 64, 512, 1.5, 0.41, 0.20},
+                               {kTile64Split, 64, 256, 2.3, 0.24, 0.16},
+                               {kTile128, 128, 512, 3.6, 0.88, 0.67},
+                               {kTile128Deep, 128, 256, 2.2, 0.62, 0.50},
+                               {kTile256, 256, 256, 6.2, 1.38, 1.25}};
 
-int pick_tile(const MatmulArgs& p, bool grouped, bool widest)
+Form pick_form(const MatmulArgs& p, bool grouped, bool widest)
 {
     const int64_t columns16 = ceil_div(p.N, 16), slabs = ceil_div(p.kbytes, kSlab);
-    if (grouped ? (ceil_div(p.M, 16) + std::min(p.E, p.M)) * columns16 <= 512 : p.M <= 16 || ceil_div(p.M, 16) * columns16 <= 512) return 0;
-    int best = 0;
+    if (grouped ? (ceil_div(p.M, 16) + std::min(p.E, p.M)) * columns16 <= 512 : p.M <= 16 || ceil_div(p.M, 16) * columns16 <= 512) return kRows;
+    Form best = kRows;
     double least = 0.0;
-    for (int i = 0; i < (widest ? 3 : 2); ++i) {
-        const TileTime& t = kTiles[i];
+    for (const TileTime& t : kTiles) {
+        if (t.form == kTile256 && !widest) continue;
         const double rows = (double)ceil_div(p.M, t.size) + (grouped ? 0.5 * p.E : 0.0);
         const double tiles = std::ceil(rows) * (double)ceil_div(p.N, t.size);
         const double full = std::floor(tiles / t.places), rest = tiles - full * t.places;
         const double last = rest == 0.0 ? 0.0 : rest <= 0.5 * t.places ? t.slab_half_empty : t.slab;
         const double time = std::max(7.2, 3.0 + slabs * (full * t.slab + last) + (full + (rest > 0.0)) * t.start);
-        if (i == 0 || time < least) best = t.size, least = time;
+        if (best == kRows || time < least) best = t.form, least = time;
     }
     return best;
 }
@@ -55,10 +61,12 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch(const MatmulArgs& p, 
 {
     // (32-bit results of codes keep both operands widened in registers: the widest tile has none left)
     constexpr bool WIDEST = AT != SC_ELEM_E4M3 || YT != SC_ELEM_F32;
-    switch (pick_tile(p, GROUPED, WIDEST)) {
-        case 0: return launch_rows<AT, YT, GROUPED>(p, stream);
-        case 64: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 4>(p, stream);
-        case 128: return launch_tile<AT, YT, GROUPED, 128, 128, 2, 2, 2>(p, stream);
+    switch (pick_form(p, GROUPED, WIDEST)) {
+        case kRows: return launch_rows<AT, YT, GROUPED>(p, stream);
+        case kTile64: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 4>(p, stream);
+        case kTile64Split: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 3, 2>(p, stream);
+        case kTile128: return launch_tile<AT, YT, GROUPED, 128, 128, 2, 2, 2>(p, stream);
+        case kTile128Deep: return launch_tile<AT, YT, GROUPED, 128, 128, 4, 2, 4>(p, stream);
         default: break;
     }
     if constexpr (WIDEST) return launch_tile<AT, YT, GROUPED, 256, 256, 4, 2, 2>(p, stream);

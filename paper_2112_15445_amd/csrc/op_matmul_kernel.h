@@ -203,9 +203,11 @@ template <int N> __device__ __forceinline__ void staged()
 }
 
 // BT x BN of y per workgroup, WT x WN waves, ST slabs in LDS: one is multiplied while the ST - 1 behind it arrive.
+// KS groups of such waves take every KS-th slab each, all in step, and the first adds the sums of the others to its own in their order:
+// where there are fewer workgroups than compute units, what a slab takes is the way from barrier to barrier, not its arithmetic.
 // AT: type of the operands, YT: of y.
-template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN, int ST>
-__global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs p)
+template <int AT, int YT, bool GROUPED, int BT, int BN, int WT, int WN, int ST, int KS>
+__global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(MatmulArgs p)
 {
     constexpr int W = WT * WN, TF = BT / WT / 16, NF = BN / WN / 16;    // waves; 16-row products of a wave along the rows / columns of y
     constexpr int AI = BT / 8 / W, BI = BN / 8 / W;                     // copies of 1 KB (eight rows) a wave makes of a slab
@@ -214,8 +216,11 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
     constexpr int kCopies = AI + BI + (CODES ? 1 : 0);                  // of a wave and slab
     static_assert(AI * 8 * W == BT && BI * 8 * W == BN && NF % 2 == 0, "tile");
     static_assert(!CODES || (BT + (BN + 127) / 128 <= W * 64), "one lane fetches a scale");
-    __shared__ __align__(16) uint8_t lds[ST * (kStage + kScales)];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int kAll = ST * KS * kStage;                              // the scales lie behind the slabs
+    __shared__ __align__(16) uint8_t lds[ST * KS * (kStage + kScales)];
+    static_assert((KS - 1) * W * NF * TF * 1024 <= sizeof(lds), "the groups' sums");
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = KS > 1 ? all / W : 0, wave = KS > 1 ? all % W : all, tid = wave * 64 + lane;      // group of waves, place in it
     const int ntn = (p.N + BN - 1) / BN;
 
     // The place of this workgroup: neighbours in the order of launch go to different XCDs, so the ids are dealt out again such
@@ -279,21 +284,23 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
 
     // Slabs: a last, short one comes first (it is masked on its way through registers), then the whole ones in their order.
     const int whole = p.kbytes / kSlab, tail = p.kbytes % kSlab, slabs = whole + (tail != 0);
-    auto copy = [&](int i, int s, int buf) {  // copy i of whole slab s
-        const uint32_t at = lds0 + buf * kStage;
+    const int turns = (slabs + KS - 1) / KS, mine = (slabs - kg + KS - 1) / KS;      // of all groups; slabs of this one
+    auto copy = [&](int i, int turn, int buf) {  // copy i of this group's whole slab of a turn
+        const int s = turn * KS + kg - (tail != 0);
+        const uint32_t at = lds0 + (buf * KS + kg) * kStage;
         if (i < BI) to_lds<16>(uniform(bbase + s * kSlab), boff[i], at + BT * kSlab + (wave + i * W) * 1024);
         else if (i < BI + AI) {
             const int j = i - BI;
             if constexpr (GROUPED) to_lds_ptr<16>(aptr[j] + s * kSlab, at + (wave + j * W) * 1024);
             else to_lds<16>(uniform(abase + s * kSlab), aoff[j], at + (wave + j * W) * 1024);
-        } else to_lds_ptr<4>(sptr + s * 4, lds0 + ST * kStage + buf * kScales + wave * 256);
+        } else to_lds_ptr<4>(sptr + s * 4, lds0 + kAll + (buf * KS + kg) * kScales + wave * 256);
     };
-    auto stage = [&](int s, int buf) {
+    auto stage = [&](int turn) {
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy(i, s, buf);
+        for (int i = 0; i < kCopies; ++i) copy(i, turn, turn);
     };
-    const int ahead = min(ST - 1, slabs);
-    if (tail) {
+    const int ahead = min(ST - 1, mine);
+    if (tail && kg == 0) {
         v4i part[AI + BI];
         int have[AI + BI];                   // bytes of the short slab from a lane's chunk on
         float scale = 0.0f;
@@ -315,15 +322,15 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             if (have[i] > 0) part[i] = *reinterpret_cast<const v4i*>(row + whole * kSlab + chunk);
         }
         if constexpr (CODES) scale = *reinterpret_cast<const float*>(sptr + whole * 4);
-        for (int s = 1; s < ahead; ++s) stage(s - 1, s);
+        for (int s = 1; s < ahead; ++s) stage(s);
 #pragma unroll
         for (int i = 0; i < AI + BI; ++i) {
             const bool of_a = i < AI;
             *reinterpret_cast<v4i*>(lds + (of_a ? 0 : BT * kSlab) + (wave + (of_a ? i : i - AI) * W) * 1024 + lane * 16) = first_bytes(part[i], have[i]);
         }
-        if constexpr (CODES) *reinterpret_cast<float*>(lds + ST * kStage + tid * 4) = scale;
+        if constexpr (CODES) *reinterpret_cast<float*>(lds + kAll + tid * 4) = scale;
     } else {
-        for (int s = 0; s < ahead; ++s) stage(s, s);
+        for (int s = 0; s < ahead; ++s) stage(s);
     }
 
     const int wt = wave % WT, wn = wave / WT;
@@ -335,13 +342,12 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
     // A slab is NF steps: one operand of the weights against the TF of a.  The weights are read two steps ahead, and a block's sums
     // are scaled and added under the matrix instructions of the step behind it.
     int buf = 0, next = (ST - 1) % ST;
-    // Slab `it`; MORE: the copies of slab it + ST - 1 are made in its first steps (a wave that issues them all at once waits for the
+    // This group's slab of turn `it`; MORE: the copies of turn it + ST - 1 are made in its first steps (a wave that issues them all at once waits for the
     // others', and late ones hold up the next slab).
     auto slab = [&](auto more, int it) {
         constexpr bool MORE = decltype(more)::value;
         constexpr int kSpread = NF > 2 ? NF / 2 : NF;
-        const int coming = it + ST - 1 - (tail != 0);
-        const uint8_t* A = lds + buf * kStage;
+        const uint8_t* A = lds + (buf * KS + kg) * kStage;
         const uint8_t* Bm = A + BT * kSlab;
         v4i t[TF][2], w[3][2];
         v4f d[2][TF];
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             for (int h = 0; h < 2; ++h) t[j][h] = *reinterpret_cast<const v4i*>(A + (trow + 16 * j) * kSlab + (((2 * q + h) ^ key) << 4));
         if (NF > 1) read_w(1);
         if constexpr (CODES) {
-            const float* S = reinterpret_cast<const float*>(lds + ST * kStage + buf * kScales);
+            const float* S = reinterpret_cast<const float*>(lds + kAll + (buf * KS + kg) * kScales);
             sw = S[BT + (wn * NF * 16) / 128];
 #pragma unroll
             for (int j = 0; j < TF; ++j) sc[j] = S[trow + 16 * j];
@@ -373,7 +379,7 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
             if constexpr (MORE)
                 if (i < kSpread)
 #pragma unroll
-                    for (int u = i * kCopies / kSpread; u < (i + 1) * kCopies / kSpread; ++u) copy(u, coming, next);
+                    for (int u = i * kCopies / kSpread; u < (i + 1) * kCopies / kSpread; ++u) copy(u, it + ST - 1, next);
             if (CODES && i == 1)
 #pragma unroll
                 for (int j = 0; j < TF; ++j) sc[j] *= sw;
@@ -411,13 +417,30 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void matmul_tile_kernel(MatmulArgs
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
     int it = 0;
-    for (; it + ST - 1 < slabs; ++it) {
+    for (; it + ST - 1 < mine; ++it) {
         staged<(ST - 2) * kCopies>();
         slab(yes, it);
     }
-    for (; it < slabs; ++it) {
+    for (; it < turns; ++it) {               // (every group comes to every barrier)
         staged<0>();
-        slab(no, it);
+        if (KS == 1 || it < mine) slab(no, it);
+    }
+    if constexpr (KS > 1) {
+        v4f* sums = reinterpret_cast<v4f*>(lds) + wave * NF * TF * 64 + lane;
+        __syncthreads();
+        if (kg > 0)
+#pragma unroll
+            for (int i = 0; i < NF; ++i)
+#pragma unroll
+                for (int j = 0; j < TF; ++j) sums[((kg - 1) * W * NF * TF + i * TF + j) * 64] = acc[i][j];
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+            for (int i = 0; i < NF; ++i)
+#pragma unroll
+                for (int j = 0; j < TF; ++j) acc[i][j] += sums[(k * W * NF * TF + i * TF + j) * 64];
     }
 
     // y: a lane has eight neighbouring columns per pair of products.

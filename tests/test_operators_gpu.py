@@ -262,11 +262,32 @@ def scale_table(scale, row):
     return t.cuda()
 
 
+FORMS = ["rows", "64", "64 split", "128", "128 deep", "256"]
+
+
+def product_form(M, N, kbytes, E=0, widest=True):
+    """The form that a product runs in: the estimate of csrc/op_matmul.hip."""
+    cd = lambda a, b: -(-a // b)  # noqa: E731
+    slabs, w = cd(kbytes, 128), (cd(M, 16) + min(E, M)) * cd(N, 16)
+    if w <= 512 or (not E and M <= 16):
+        return "rows"
+    best = None
+    for form, size, places, start, slab, half in (("64", 64, 512, 1.5, 0.41, 0.20), ("64 split", 64, 256, 2.3, 0.24, 0.16), ("128", 128, 512, 3.6, 0.88, 0.67),
+                                                  ("128 deep", 128, 256, 2.2, 0.62, 0.50), ("256", 256, 256, 6.2, 1.38, 1.25)):
+        if form == "256" and not widest:
+            continue
+        full, rest = divmod(int(np.ceil(cd(M, size) + 0.5 * E)) * cd(N, size), places)
+        t = max(7.2, 3.0 + slabs * (full * slab + (0 if rest == 0 else half if rest <= places / 2 else slab)) + (full + (rest > 0)) * start)
+        if best is None or t < best[0]:
+            best = (t, form)
+    return best[1]
+
+
 MATMUL_SHAPES = [  # M, N, K
     (1, 1, 1), (1, 16, 128), (1, 100, 300), (1, 512, 4096), (1, 2049, 640), (2, 64, 1000), (3, 130, 17), (8, 1024, 512), (15, 200, 129), (16, 256, 2048),
     (17, 257, 256), (32, 96, 1100), (33, 512, 384), (64, 64, 64), (65, 130, 100), (100, 1000, 260), (127, 128, 128), (129, 300, 300),
     (200, 2048, 512), (256, 256, 256), (257, 511, 640), (333, 1000, 1100), (700, 70, 900), (1000, 1030, 129), (2100, 520, 272),
-    (4100, 4100, 272),
+    (4100, 4100, 272), (300, 700, 3000), (1500, 900, 1300), (2000, 1100, 1000),
 ]
 
 
@@ -291,6 +312,35 @@ def test_matmul_blocks(M, N, K, y_type):
     ref, bound = O.product(O.values(ca, sa, 1), O.values(cb, sb, 128), bias, kind, cores8=y_type != "f32")
     assert_close(host(y.rows()), ref, bound, y_type, (M, N, K, kind))
     y.check_guard()
+
+
+@pytest.mark.parametrize("y_type", ["f16", "bf16"])
+def test_matmul_blocks_on_the_widest_tile(y_type):
+    """Rows picked all over the matrix against the definition; the sizes are not multiples of anything."""
+    M, N, K = 4090, 4090, 1100
+    assert product_form(M, N, K) == "256"
+    rng = np.random.default_rng(5)
+    kb, row = -(-K // 128), -(-K // 16) * 16
+    ra, ca, sa = code_matrix(rng, M, K, 1, row)
+    rb, cb, sb = code_matrix(rng, N, K, 128, row, 0.05)
+    bias = (0.2 * rng.normal(size=N)).astype(np.float32)
+    a, b, asc, bsc, bd = ra.cuda(), rb.cuda(), scale_table(sa, kb), scale_table(sb, kb), torch.from_numpy(bias).cuda()
+    y = Out(M, N, y_type)
+    op = B.BlockMatmul(M, N, K, y_type=T[y_type], act="silu", a_row=row, b_row=row)
+    ws, wp, wn = workspace(op)
+    op.forward(a.data_ptr(), asc.data_ptr(), b.data_ptr(), bsc.data_ptr(), bd.data_ptr(), y.ptr, wp, wn, stream())
+    torch.cuda.synchronize()
+    at = sorted(set(range(0, M, 41)) | set(range(250, 262)) | set(range(M - 5, M)))
+    ref, bound = O.product(O.values(ca[at], sa[at], 1), O.values(cb, sb, 128), bias, "silu", cores8=True)
+    assert_close(host(y.rows()[at]), ref, bound, y_type, (M, N, K))
+    y.check_guard()
+
+
+def test_every_form_of_the_products_is_looked_at():
+    """The shapes of the tests reach every form in every type (32-bit results of codes have no widest tile)."""
+    whole = {product_form(M, N, K) for M, N, K in MATMUL_SHAPES} | {"256"}
+    assert whole == set(FORMS)
+    assert {product_form(M, N, K, widest=False) for M, N, K in MATMUL_SHAPES} == set(FORMS[:-1])
 
 
 def test_matmul_blocks_twice_gives_the_same_bits():
@@ -348,8 +398,8 @@ GROUPS = {  # what each expert gets
 }
 
 
-def run_grouped(rng, counts, N, K, a_type, y_type, kind, gather, bias, odd, first=0, beyond=0):
-    """One call with `first` rows before the first group and `beyond` behind the last; the rows that the groups cover, what came
+def run_grouped(rng, counts, N, K, a_type, y_type, kind, gather, bias, odd, first=0, beyond=0, some=1):
+    """One call with `first` rows before the first group and `beyond` behind the last (some: see below); the rows that the groups cover, what came
     out, the exact result and its bound."""
     E, T_ = len(counts), sum(counts)
     M = first + T_ + beyond
@@ -390,8 +440,9 @@ def run_grouped(rng, counts, N, K, a_type, y_type, kind, gather, bias, odd, firs
     ref, bound = np.zeros((M, N)), np.zeros((M, N))
     for e in range(E):
         lo, hi = offsets[e], offsets[e + 1]
-        if hi > lo:
-            ref[lo:hi], bound[lo:hi] = O.product(av[lo:hi], bv[e], None if bias_h is None else bias_h[e], kind, blocks=codes, cores8=codes and y_type != "f32")
+        if hi > lo:                                           # (some > 1: each some-th row and the ends)
+            at = sorted(set(range(lo, hi, some)) | {lo, hi - 1})
+            ref[at], bound[at] = O.product(av[at], bv[e], None if bias_h is None else bias_h[e], kind, blocks=codes, cores8=codes and y_type != "f32")
     return range(first, first + T_), y, ref, bound
 
 
@@ -400,7 +451,7 @@ def run_grouped(rng, counts, N, K, a_type, y_type, kind, gather, bias, odd, firs
 def test_matmul_grouped(groups, a_type, y_type):
     counts = GROUPS[groups]
     rng = np.random.default_rng(len(groups) * 31 + sum(counts))
-    for i, (N, K) in enumerate(((64, 128), (130, 200), (257, 520), (1, 1), (512, 1024)) if groups != "thousands" else ((2060, 200), (2048, 128))):
+    for i, (N, K) in enumerate(((64, 128), (130, 200), (257, 520), (1, 1), (512, 1024)) if groups != "thousands" else ((2060, 200), (2048, 128), (300, 1200))):
         if groups == "many" and K > 600:
             continue
         gather, bias, odd = (i + len(counts)) % 2 == 1, i % 3 == 1, i % 2
@@ -410,6 +461,28 @@ def test_matmul_grouped(groups, a_type, y_type):
         got = host(y.rows())
         assert_close(got[covered.start:covered.stop], ref[covered.start:covered.stop], bound[covered.start:covered.stop], y_type, (groups, N, K, kind))
         y.check_guard(covered)
+
+
+@pytest.mark.parametrize("a_type,y_type", [("f16", "f16"), ("bf16", "f32"), ("e4m3", "bf16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("form", FORMS[1:])
+def test_matmul_grouped_in_every_form(form, a_type, y_type):
+    """Unequal groups in each of the tiles, rows picked by an index, some of which stand for zeros; every 17th row and the ends of the
+    groups against the definition."""
+    codes = a_type == "e4m3"
+    # (columns, summed bytes, rows of the groups)
+    N, kbytes, counts = {"64": (700, 400, [300, 0, 900, 401]), "64 split": (330, 3300, [200, 0, 300, 101]), "128": (2060, 400, [1500, 0, 2700, 3999]),
+                         "128 deep": (1000, 2500, [700, 0, 1000, 901]), "256": (4090, 2400, [900, 0, 1200, 1197])}[form]
+    if form == "256" and codes and y_type == "f32":
+        return
+    K = kbytes // (1 if codes else 2)
+    assert product_form(sum(counts), N, kbytes, len(counts), not (codes and y_type == "f32")) == form
+    rng = np.random.default_rng(len(form))
+    covered, y, ref, bound = run_grouped(rng, counts, N, K, a_type, y_type, "silu", True, True, 0, some=17)
+    at = ref.any(1) | bound.any(1)
+    assert at.sum() > sum(counts) // 17
+    got = host(y.rows())
+    assert_close(got[at], ref[at], bound[at], y_type, (form, a_type, y_type))
+    y.check_guard(covered)
 
 
 def test_matmul_grouped_with_offsets_that_are_out_of_range():
