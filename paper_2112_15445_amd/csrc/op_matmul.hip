@@ -65,7 +65,9 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch(const MatmulArgs& p, 
         case kRows: return launch_rows<AT, YT, GROUPED>(p, stream);
         case kTile64: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 4>(p, stream);
         case kTile64Split: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 3, 2>(p, stream);
-        case kTile128: return launch_tile<AT, YT, GROUPED, 128, 128, 2, 2, 2>(p, stream);
+        // (eight waves where their registers leave room for a second workgroup: 3 % less than four over 68 products; 7 % more in 32-bit
+        // results of codes)
+        case kTile128: return launch_tile<AT, YT, GROUPED, 128, 128, WIDEST ? 4 : 2, 2, 2>(p, stream);
         case kTile128Deep: return launch_tile<AT, YT, GROUPED, 128, 128, 4, 2, 4>(p, stream);
         default: break;
     }
