@@ -48,6 +48,9 @@ template <int V> __device__ __forceinline__ void load_params(float* out, const f
     }
 }
 
+// floor(i / d) for 0 <= i < 2^19, inv = 1.0f / d: the half keeps the product away from whole numbers by more than it is rounded.
+__device__ __forceinline__ int small_div(int i, float inv) { return (int)(((float)i + 0.5f) * inv); }
+
 // y of V neighbouring channels of one position; gam: gamma over the spread.
 template <int ACT, int V>
 __device__ __forceinline__ void finish(float* f, const float* mean, const float* gam, const float* bet, int have)
@@ -164,16 +167,13 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
 {
     constexpr int V = kVec<XT>, U = 8;
     __shared__ float ms[kThreads * V], qs[kThreads * V], ns[kThreads];
-    int id = blockIdx.x;
-    const int sg = id % a.segs;
-    id /= a.segs;
-    const int st = id % a.stretches, n = id / a.stretches;
+    const int n = blockIdx.x, st = blockIdx.y, sg = blockIdx.z;
     // (a.parts > 1: a segment is a part of one group; else whole groups)
     const int g0 = a.parts > 1 ? sg / a.parts : sg * (a.seg / a.Cg), part = a.parts > 1 ? sg % a.parts : 0;
     const int c0 = a.parts > 1 ? g0 * a.Cg + part * a.seg : sg * a.seg;
     const int cn = a.parts > 1 ? min(a.seg, a.Cg - part * a.seg) : min(a.seg, a.C - c0);
-    const int tpr = (cn + V - 1) / V, R = kThreads / tpr;
-    const int r = threadIdx.x / tpr, v = threadIdx.x - r * tpr;
+    const int tpr = (cn + V - 1) / V, R = small_div(kThreads, 1.0f / (float)tpr);
+    const int r = small_div(threadIdx.x, 1.0f / (float)tpr), v = threadIdx.x - r * tpr;
     const int p0 = st * a.len, pn = min(a.len, a.S - p0);
     const int have = min(V, cn - v * V);
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + p0 * a.x_row + c0 + v * V;
@@ -233,17 +233,17 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
     // Sixteen lanes put a group together: the mean of the means, then the deviations around it.
     const int groups = a.parts > 1 ? 1 : cn / a.Cg, gc = a.parts > 1 ? cn : a.Cg;
     const int sub = threadIdx.x >> 4, sl = threadIdx.x & 15;
-    const float total = (float)pn * (float)gc;
+    const float total = (float)pn * (float)gc, inv_gc = 1.0f / (float)gc;
     for (int g = sub; g < groups; g += kThreads / 16) {
         float s = 0.0f;
         for (int i = sl; i < R * gc; i += 16) {
-            const int rr = i / gc, cc = g * gc + (i - rr * gc);
+            const int rr = small_div(i, inv_gc), cc = g * gc + (i - rr * gc);
             s += ns[rr * tpr + cc / V] * ms[rr * tpr * V + cc];
         }
         const float m = sum16(s) / total;
         float q = 0.0f;
         for (int i = sl; i < R * gc; i += 16) {
-            const int rr = i / gc, cc = g * gc + (i - rr * gc);
+            const int rr = small_div(i, inv_gc), cc = g * gc + (i - rr * gc);
             const float d = ms[rr * tpr * V + cc] - m;
             q += qs[rr * tpr * V + cc] + ns[rr * tpr + cc / V] * d * d;
         }
@@ -254,18 +254,15 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
 
 // The second: one workgroup per (sample, a.rows positions, up to kThreads * V channels).  Codes: a row's lanes are padded to whole
 // blocks of 128 channels, so that a block's lanes are neighbours in one wave.
-template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, int wide, int wides, int chunks)
+template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a, int wide)
 {
     constexpr int V = kVec<XT>, U = 4, L = kQBlock / V;
     constexpr bool CODES = YT == SC_ELEM_E4M3;
     extern __shared__ float2 gs[];           // mean, 1 / spread of the groups of this workgroup
-    int id = blockIdx.x;
-    const int sg = id % wides;
-    id /= wides;
-    const int ch = id % chunks, n = id / chunks;
+    const int n = blockIdx.x, ch = blockIdx.y, sg = blockIdx.z;
     const int c0 = sg * wide, cn = min(wide, a.C - c0);
     const int tpr = CODES ? (cn + kQBlock - 1) / kQBlock * L : (cn + V - 1) / V;
-    const int R = kThreads / tpr, r = threadIdx.x / tpr, v = threadIdx.x - r * tpr;
+    const int R = small_div(kThreads, 1.0f / (float)tpr), r = small_div(threadIdx.x, 1.0f / (float)tpr), v = threadIdx.x - r * tpr;
     const int have = min(V, cn - v * V), c = c0 + v * V;
     const int p0 = ch * a.rows, p1 = r < R ? min(a.S, p0 + a.rows) : 0;
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
@@ -450,11 +447,11 @@ template <int XT, int YT, int ACT> sc_status_t launch_norm(const sc_group_norm_t
         return launched();
     }
     const int64_t first = (int64_t)d->N * s.segs * s.stretches, second = (int64_t)d->N * s.wides * s.chunks;
-    if (std::max(first, second) * kThreads >= (int64_t)1 << 32) return SC_ERR_RANGE;
-    norm_stats_kernel<XT><<<dim3((unsigned)first), kThreads, 0, stream>>>(a);
+    if (std::max(first, second) * kThreads >= (int64_t)1 << 32 || std::max({s.segs, s.wides, s.chunks}) > 65535) return SC_ERR_RANGE;
+    norm_stats_kernel<XT><<<dim3((unsigned)d->N, (unsigned)s.stretches, (unsigned)s.segs), kThreads, 0, stream>>>(a);
     if (launched() != SC_OK) return SC_ERR_HIP;
     const size_t lds = (size_t)std::min<int64_t>(d->G, ceil_div(s.wide, a.Cg) + 1) * sizeof(float2);
-    norm_apply_kernel<XT, YT, ACT><<<dim3((unsigned)second), kThreads, lds, stream>>>(a, s.wide, s.wides, s.chunks);
+    norm_apply_kernel<XT, YT, ACT><<<dim3((unsigned)d->N, (unsigned)s.chunks, (unsigned)s.wides), kThreads, lds, stream>>>(a, s.wide);
     return launched();
 }
 

@@ -195,3 +195,25 @@ def test_a_wrong_scale_block_is_seen():
                   O.product(O.values(ca, sa, 1)[:, :-1], O.values(cb, sb, 128)[:, :-1])[0]):
         assert O.excess(wrong, ref, bound, "f32")[0] > 0 and O.excess(wrong, ref, bound, "bf16")[0] > 0
     assert O.excess(ref, ref, bound, "f32")[0] <= 0
+
+
+def test_operator_kernels_spill_at_most_two_registers():
+    """No scratch memory but in the widest group norm form that leaves codes of two-byte inputs (two registers of it)."""
+    import re
+
+    import test_kernel_resources as R
+    with open(B.LIB_PATH, "rb") as f:
+        data = f.read()
+    seen = {}
+    for elf in R._code_objects(data):
+        for k in R._kernels(elf):
+            m = re.search(r"(matmul_tile|matmul_rows|norm_resident|norm_stats|norm_apply|quantize_rows|quantize_tiles)_kernelI", k[".name"])
+            if m:
+                seen[k[".name"]] = (m.group(1), k)
+    count = {}
+    for name, (kind, k) in seen.items():
+        count[kind] = count.get(kind, 0) + 1
+        assert k[".vgpr_spill_count"] <= (2 if kind == "norm_resident" else 0) and k[".private_segment_fixed_size"] <= (16 if kind == "norm_resident" else 0), name
+        assert k[".vgpr_count"] + k.get(".agpr_count", 0) <= 256, name
+    # types of operands and results: 10 (3 of codes whole, 7 grouped); tiles: 5 each and the widest in 8; group norm: 6 pairs, 3 activations, 4 sizes
+    assert count == {"matmul_tile": 10 * 4 + 8, "matmul_rows": 10, "norm_resident": 72, "norm_stats": 3, "norm_apply": 18, "quantize_rows": 3, "quantize_tiles": 3}
