@@ -138,6 +138,12 @@ __device__ __forceinline__ float max16(float v)
     v = fmaxf(v, row_ror<2>(v));
     return fmaxf(v, row_ror<1>(v));
 }
+__device__ __forceinline__ float sum64(float v)
+{
+    v = sum16(v);
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
 // ... over the L = 16 or 32 lanes that hold 128 values.
 template <int L> __device__ __forceinline__ float max_block(float v)
 {

@@ -3,13 +3,15 @@
 // Bound by memory: x read once (twice where it does not fit a workgroup), y written once.  Two forms:
 //
 //   one launch   a workgroup holds whole groups of one sample in its registers, all positions of them: mean, then the squared
-//                deviations from it, then the result, with no second look at memory.  Taken where that fits (norm_resident).
+//                deviations from it, then the result, with no second look at memory.  Taken where that fits: some groups of a
+//                sample (norm_resident: their lanes have to be powers of two) or the whole sample (norm_sample).
 //   two launches statistics of stretches of positions (each: mean and sum of squared deviations, put together pairwise, never as
 //                a difference of large sums), then the result, whose workgroups first put their sample's stretches together.
 //                x comes from the last-level cache the second time where it fits there (256 MB).
 #include "op_common.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace sc {
 namespace {
@@ -25,7 +27,7 @@ struct NormArgs {
     void* y;
     float* ys;
     float2* stats;                           // [N][G][stretches][parts] mean, sum of squared deviations
-    int N, S, C, G, Cg;
+    int N, S, C, G, Cg, NB;                  // (NB: blocks of 128 channels)
     int seg, segs, parts;                    // channels of a statistics workgroup, segments of C, segments of one group (1: whole groups)
     int len, stretches;                      // positions of a stretch, stretches of a sample
     int rows;                                // positions of a workgroup of the second launch
@@ -160,13 +162,138 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
+// One launch, groups of any size: a workgroup holds a whole sample, lanes side by side V neighbouring channels each.  Sums of channels go
+// through LDS and are put together by group (by_group), for the mean and then for the squared deviations from it.
+// ---------------------------------------------------------------------------------------------------------------------------
+// out[g] = the sum of value(g, row, channel of the group) over R rows and gc channels: by all T threads for one group, by a wave each
+// for a few, by sixteen lanes each for many.
+template <int T, class F> __device__ __forceinline__ void by_group(int groups, int gc, int R, float* out, float* red, F value)
+{
+    const float inv = 1.0f / (float)gc;
+    auto part = [&](int g, int first, int step) {
+        float s = 0.0f;
+        for (int i = first; i < R * gc; i += step) {
+            const int rr = small_div(i, inv);
+            s += value(g, rr, i - rr * gc);
+        }
+        return s;
+    };
+    if (groups == 1) {
+        const float s = sum64(part(0, threadIdx.x, T));
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float all = 0.0f;
+            for (int w = 0; w < T / 64; ++w) all += red[w];
+            out[0] = all;
+        }
+    } else if (groups * 16 < T) {
+        for (int g = threadIdx.x >> 6; g < groups; g += T / 64) {
+            const float s = sum64(part(g, threadIdx.x & 63, 64));
+            if ((threadIdx.x & 63) == 0) out[g] = s;
+        }
+    } else {
+        for (int g = threadIdx.x >> 4; g < groups; g += T / 16) {
+            const float s = sum16(part(g, threadIdx.x & 15, 16));
+            if ((threadIdx.x & 15) == 0) out[g] = s;
+        }
+    }
+    __syncthreads();
+}
+
+template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T, 4) void norm_sample_kernel(NormArgs a)
+{
+    constexpr int V = kVec<XT>, L = kQBlock / V;
+    constexpr bool CODES = YT == SC_ELEM_E4M3;
+    __shared__ float vals[T * V], red[T / 64];
+    extern __shared__ float by[];                    // [2][G]
+    const int n = blockIdx.x;
+    const int tpr = CODES ? a.NB * L : (a.C + V - 1) / V, R = small_div(T, 1.0f / (float)tpr);
+    const int r = small_div(threadIdx.x, 1.0f / (float)tpr), v = threadIdx.x - r * tpr, c = v * V;
+    const int have = min(V, a.C - c), rows = r < R ? a.S : 0;
+    const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
+    v4i raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        raw[u] = v4i{0, 0, 0, 0};
+        if (r + u * R < rows && have > 0) raw[u] = have == V ? load_raw<XT>(x + (r + u * R) * a.x_row) : load_raw_part<XT>(x + (r + u * R) * a.x_row, have);
+    }
+    float gam[V], bet[V];
+    load_params<V>(gam, a.gamma, c, have, 1.0f);
+    load_params<V>(bet, a.beta, c, have, 0.0f);
+    const float cnt = (float)a.S * (float)a.Cg;
+    const int first = min(c, a.C - 1) / a.Cg, ends = (first + 1) * a.Cg - c;   // the group of a lane's first channel, its channels to come
+    auto each = [&](const float* t, auto take) {     // take(i, t of the group of channel c + i)
+        int g = first, left = ends;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            take(i, t[min(g, a.G - 1)]);
+            if (--left == 0) ++g, left = a.Cg;
+        }
+    };
+    auto forget = [&] {                              // (see norm_resident_kernel)
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(raw[u]));
+    };
+    float sum[V] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[V];
+        to_floats<XT>(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] += f[i];
+    }
+    auto together = [&](float* out) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) vals[threadIdx.x * V + i] = sum[i];
+        __syncthreads();
+        by_group<T>(a.G, a.Cg, R, out, red, [&](int g, int rr, int cc) { return vals[rr * tpr * V + g * a.Cg + cc]; });
+    };
+    together(by);
+    forget();
+    float mean[V];
+    each(by, [&](int i, float t) { mean[i] = t / cnt, sum[i] = 0.0f; });
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (r + u * R < rows) {
+            float f[V];
+            to_floats<XT>(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += (f[i] - mean[i]) * (f[i] - mean[i]);
+        }
+    together(by + a.G);
+    forget();
+    each(by + a.G, [&](int i, float t) { gam[i] *= 1.0f / sqrtf(t / cnt + a.eps); });
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int pos = r + u * R;
+        if (pos >= rows) continue;                   // (the lanes of a position go on or leave together)
+        float f[V];
+        to_floats<XT>(raw[u], f);
+        finish<ACT, V>(f, mean, gam, bet, have);
+        Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c;
+        if constexpr (CODES) {
+            float amax = kAmaxFloor;
+#pragma unroll
+            for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
+            amax = max_block<L>(amax);
+            if (c < ((a.C + 15) & ~15)) store_codes<V>(y, f, kCodeMax / amax);
+            if (v % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + c / kQBlock] = amax / kCodeMax;
+        } else {
+            store_vec<YT, V>(y, f, have);
+        }
+        if constexpr (U > 4) __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
 // Two launches, the first: one workgroup per (sample, stretch of positions, segment of channels).  A lane keeps V neighbouring
 // channels and takes U positions at a time: their mean, their squared deviations from it, and both joined to what it has.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(NormArgs a)
 {
     constexpr int V = kVec<XT>, U = 8;
-    __shared__ float ms[kThreads * V], qs[kThreads * V], ns[kThreads];
+    __shared__ float ms[kThreads * V], qs[kThreads * V], ns[kThreads], red[kThreads / 64], by[2 * kThreads * V];
     const int n = blockIdx.x, st = blockIdx.y, sg = blockIdx.z;
     // (a.parts > 1: a segment is a part of one group; else whole groups)
     const int g0 = a.parts > 1 ? sg / a.parts : sg * (a.seg / a.Cg), part = a.parts > 1 ? sg % a.parts : 0;
@@ -230,26 +357,22 @@ template <int XT> __global__ __launch_bounds__(kThreads) void norm_stats_kernel(
     }
     ns[threadIdx.x] = r < R ? cnt : 0.0f;
     __syncthreads();
-    // Sixteen lanes put a group together: the mean of the means, then the deviations around it.
+    // The groups: the mean of the means, then the deviations around it.
     const int groups = a.parts > 1 ? 1 : cn / a.Cg, gc = a.parts > 1 ? cn : a.Cg;
-    const int sub = threadIdx.x >> 4, sl = threadIdx.x & 15;
-    const float total = (float)pn * (float)gc, inv_gc = 1.0f / (float)gc;
-    for (int g = sub; g < groups; g += kThreads / 16) {
-        float s = 0.0f;
-        for (int i = sl; i < R * gc; i += 16) {
-            const int rr = small_div(i, inv_gc), cc = g * gc + (i - rr * gc);
-            s += ns[rr * tpr + cc / V] * ms[rr * tpr * V + cc];
-        }
-        const float m = sum16(s) / total;
-        float q = 0.0f;
-        for (int i = sl; i < R * gc; i += 16) {
-            const int rr = small_div(i, inv_gc), cc = g * gc + (i - rr * gc);
-            const float d = ms[rr * tpr * V + cc] - m;
-            q += qs[rr * tpr * V + cc] + ns[rr * tpr + cc / V] * d * d;
-        }
-        q = sum16(q);
-        if (sl == 0) a.stats[(((int64_t)n * a.G + g0 + g) * a.stretches + st) * a.parts + part] = make_float2(m, q);
-    }
+    const float total = (float)pn * (float)gc;
+    by_group<kThreads>(groups, gc, R, by, red, [&](int g, int rr, int cc) {
+        cc += g * gc;
+        return ns[rr * tpr + cc / V] * ms[rr * tpr * V + cc];
+    });
+    for (int g = threadIdx.x; g < groups; g += kThreads) by[g] /= total;
+    __syncthreads();
+    by_group<kThreads>(groups, gc, R, by + groups, red, [&](int g, int rr, int cc) {
+        cc += g * gc;
+        const float d = ms[rr * tpr * V + cc] - by[g];
+        return qs[rr * tpr * V + cc] + ns[rr * tpr + cc / V] * d * d;
+    });
+    for (int g = threadIdx.x; g < groups; g += kThreads)
+        a.stats[(((int64_t)n * a.G + g0 + g) * a.stretches + st) * a.parts + part] = make_float2(by[g], by[groups + g]);
 }
 
 // The second: one workgroup per (sample, a.rows positions, up to kThreads * V channels).  Codes: a row's lanes are padded to whole
@@ -355,41 +478,77 @@ template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void n
     }
 }
 
+constexpr int kNumUnits = 256;                // compute units
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // of a launch: below this
+
 bool pow2(int v) { return v > 0 && (v & (v - 1)) == 0; }
 
 struct NormShape {
-    int TPR, LPG, T, U, dies;                // one launch (TPR = 0: two)
+    int T, U;                                // one launch (T = 0: two)
+    int TPR, LPG, dies;                      // ... of lanes in powers of two (TPR = 0: of whole samples)
     int seg, segs, parts, len, stretches;    // the statistics
     int wide, wides, rows, chunks;           // the result
     size_t bytes;
 };
 
-// One launch: groups of a power of two of 16-byte lanes, all positions of a workgroup's channels in 16 vectors a lane of 1024.  The
-// channels of a workgroup make whole 128-byte lines where that fits, else the most that fits, down to 32 bytes (codes: whole
-// blocks of 128 channels always).
-bool norm_resident(const sc_group_norm_t* d, NormShape* s)
+// What a form takes, in microseconds: one launch 4.5 (of whole samples 5.5), two 11.5; then the larger of what memory takes at 4.5 TB/s
+// and, for one launch, what the fullest of 256 compute units takes at 5500 values a microsecond (three passes of 17 vector instructions in
+// all for each value).  Measured for estimated: 64 x 49 x 1040 (16 groups, f16) 15.7 for 14.8, 7 x 837 x 360 to codes 13.9 for 13.8,
+// 4 x 3000 x 416 17.5 for 18.2; 1 x 3136 x 64 (8 groups, f16) 11.3 in four workgroups, in two 15.8.
+double norm_time(const sc_group_norm_t* d, double base, double workgroups, double values, double reads)
 {
-    const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G, most = 1024 * 16;
+    const double total = (double)d->N * d->S * d->C;
+    return base + std::max(std::ceil(workgroups / kNumUnits) * values / 5500.0, total * (reads * elem_bytes(d->x_type) + elem_bytes(d->y_type)) / 4.5e6);
+}
+
+// One launch: groups of a power of two of 16-byte lanes, all positions of a workgroup's channels in 16 vectors a lane of 1024.  The
+// channels of a workgroup make a whole line of 128 bytes, or a part of one of at least 32 (codes: whole blocks of 128 channels): the
+// part of a line that the other workgroups need is read again, but where a die has all of them (`dies`).
+bool norm_resident(const sc_group_norm_t* d, NormShape* s, double* time)
+{
+    const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G;
     const bool codes = d->y_type == SC_ELEM_E4M3;
     if (Cg % V || !pow2(Cg / V) || Cg / V > 64) return false;
-    const int LPG = Cg / V, line = codes ? kQBlock / V : 8;
-    int TPR = LPG;
-    while (TPR < line && d->C % (2 * TPR * V) == 0 && (codes || TPR < 2 || (int64_t)d->S * TPR * 2 <= most)) TPR *= 2;
-    if (TPR > 64 || (codes && TPR % line) || (TPR < 2 && d->C != TPR * V)) return false;
-    const int64_t vectors = (int64_t)d->S * TPR;
-    if (vectors > most) return false;
-    s->TPR = TPR;
-    s->LPG = LPG;
-    s->T = vectors <= 256 * 4 ? 256 : vectors <= 512 * 16 ? 512 : 1024;
-    s->U = vectors <= s->T * 4 ? 4 : 16;
-    s->dies = d->N >= 16 || d->N == 8;
-    return true;
+    const int LPG = Cg / V, line = codes ? kQBlock / V : 8, least = codes ? line : d->C == V ? 1 : 2;
+    const bool dies = d->N >= 16 || d->N == 8;
+    bool any = false;
+    for (int TPR = LPG; TPR <= std::max(line, LPG) && d->C % (TPR * V) == 0; TPR *= 2) {
+        const int64_t vectors = (int64_t)d->S * TPR;
+        if (TPR < least || TPR % (codes ? line : 1) || vectors > 1024 * 16) continue;
+        const double t = norm_time(d, 4.5, (double)d->N * d->C / (TPR * V), (double)vectors * V, dies ? 1.0 : std::max(1.0, 8.0 / TPR));
+        if (ceil_div(d->N, 8) * 8 * (d->C / (TPR * V)) * 1024 >= kMaxThreads || (any && t > *time)) continue;      // (level: the wider)
+        any = true;
+        *time = t;
+        s->TPR = TPR;
+        s->LPG = LPG;
+        s->dies = dies;
+        s->T = vectors <= 256 * 4 ? 256 : vectors <= 512 * 16 ? 512 : 1024;
+        s->U = vectors <= s->T * 4 ? 4 : 16;
+    }
+    return any;
+}
+
+// One launch, a sample a workgroup: a sample in eight vectors a lane of 1024.
+bool norm_sample(const sc_group_norm_t* d, NormShape* s, double* time)
+{
+    const int V = 16 / elem_bytes(d->x_type), L = kQBlock / V;
+    const int64_t tpr = d->y_type == SC_ELEM_E4M3 ? ceil_div(d->C, kQBlock) * L : ceil_div(d->C, V);
+    if (tpr > 1024 || d->G > 2048 || (int64_t)d->N * 1024 >= kMaxThreads) return false;
+    s->T = tpr <= 256 && 256 / tpr * 4 >= d->S ? 256 : 1024;
+    s->U = s->T / tpr * 4 >= d->S ? 4 : 8;
+    *time = norm_time(d, 5.5, d->N, (double)d->S * d->C, 1.0);
+    return s->T / tpr * s->U >= d->S;
 }
 
 NormShape norm_shape(const sc_group_norm_t* d)
 {
+    if (d->N == 0 || d->S == 0) return {};
+    double best = norm_time(d, 11.5, 0.0, 0.0, 2.0), time = 0.0;
+    NormShape one{}, resident{}, sample{};
+    if (norm_resident(d, &resident, &time) && time < best) one = resident, best = time;
+    if (norm_sample(d, &sample, &time) && time < best) one = sample;
+    if (one.T) return one;
     NormShape s{};
-    if (d->N == 0 || d->S == 0 || norm_resident(d, &s)) return s;
     const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G, most = kThreads * V;
     if (Cg <= most) {
         s.seg = std::min(d->G, most / Cg) * Cg;
@@ -436,10 +595,16 @@ sc_status_t check_norm(const sc_group_norm_t* d)
 
 template <int XT, int YT, int ACT> sc_status_t launch_norm(const sc_group_norm_t* d, const NormShape& s, const NormArgs& a, hipStream_t stream)
 {
-    if (s.TPR) {
-        const int64_t blocks = (s.dies ? ceil_div(d->N, 8) * 8 : (int64_t)d->N) * (d->C / (s.TPR * kVec<XT>));
-        if (blocks * s.T >= (int64_t)1 << 32) return SC_ERR_RANGE;
-        const dim3 grid((unsigned)blocks);
+    if (s.T && !s.TPR) {
+        const size_t lds = (size_t)d->G * 2 * sizeof(float);
+        const dim3 grid((unsigned)d->N);
+        if (s.T == 256) norm_sample_kernel<XT, YT, ACT, 256, 4><<<grid, 256, lds, stream>>>(a);
+        else if (s.U == 4) norm_sample_kernel<XT, YT, ACT, 1024, 4><<<grid, 1024, lds, stream>>>(a);
+        else norm_sample_kernel<XT, YT, ACT, 1024, 8><<<grid, 1024, lds, stream>>>(a);
+        return launched();
+    }
+    if (s.T) {
+        const dim3 grid((unsigned)((s.dies ? ceil_div(d->N, 8) * 8 : (int64_t)d->N) * (d->C / (s.TPR * kVec<XT>))));
         if (s.T == 256) norm_resident_kernel<XT, YT, ACT, 256, 4><<<grid, 256, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
         else if (s.U == 4) norm_resident_kernel<XT, YT, ACT, 512, 4><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
         else if (s.T == 512) norm_resident_kernel<XT, YT, ACT, 512, 16><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
@@ -496,7 +661,7 @@ extern "C" sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const vo
     NormArgs a;
     a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.ys = y_scale;
     a.stats = static_cast<float2*>(workspace_dev);
-    a.N = d->N; a.S = d->S; a.C = d->C; a.G = d->G; a.Cg = d->C / d->G;
+    a.N = d->N; a.S = d->S; a.C = d->C; a.G = d->G; a.Cg = d->C / d->G; a.NB = (int)ceil_div(d->C, kQBlock);
     a.seg = shape.seg; a.segs = shape.segs; a.parts = shape.parts; a.len = shape.len; a.stretches = shape.stretches; a.rows = shape.rows;
     a.eps = d->eps;
     // (32 x 56x56 x 256 fp32, 206 MB: 47 us with the hint and 52 without; 39 MB of a quantiser's: 11.0 with and 10.4 without)

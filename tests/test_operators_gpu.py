@@ -120,6 +120,8 @@ NORM_SHAPES = [  # N, S, C, G, extra elements between positions, elements before
     (1, 1, 32, 32, 0, 0), (1, 1, 64, 8, 0, 0), (2, 49, 2048, 32, 0, 0), (3, 7, 100, 10, 0, 0), (2, 37, 360, 30, 8, 0),
     (1, 837, 360, 30, 0, 0), (2, 64, 96, 1, 3, 1), (1, 3000, 64, 32, 0, 0), (5, 16, 30, 30, 2, 0), (1, 5000, 7, 1, 0, 1),
     (2, 3136, 256, 32, 0, 0), (1, 196, 1024, 16, 8, 8), (33, 5, 24, 3, 0, 0),
+    (2, 4, 844, 1, 0, 0), (3, 1, 7, 7, 0, 0), (2, 300, 130, 13, 0, 0), (2, 90, 520, 4, 3, 1), (1, 1000, 52, 2, 0, 0), (2, 20, 2040, 1020, 0, 0), (1, 2, 6000, 3000, 0, 0),
+    (1, 700, 5000, 2, 0, 0), (1, 900, 700, 700, 0, 0),
 ]
 
 

@@ -217,3 +217,16 @@ def test_operator_kernels_spill_at_most_two_registers():
         assert k[".vgpr_count"] + k.get(".agpr_count", 0) <= 256, name
     # types of operands and results: 10 (3 of codes whole, 7 grouped); tiles: 5 each and the widest in 8; group norm: 6 pairs, 3 activations, 4 sizes
     assert count == {"matmul_tile": 10 * 4 + 8, "matmul_rows": 10, "norm_resident": 72, "norm_stats": 3, "norm_apply": 18, "quantize_rows": 3, "quantize_tiles": 3}
+
+
+def test_whole_sample_norm_kernels_do_not_spill():
+    import re
+
+    import test_kernel_resources as R
+    with open(B.LIB_PATH, "rb") as f:
+        data = f.read()
+    seen = {k[".name"]: k for elf in R._code_objects(data) for k in R._kernels(elf) if re.search(r"norm_sample_kernelI", k[".name"])}
+    for name, k in seen.items():
+        assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, name
+        assert k[".vgpr_count"] + k.get(".agpr_count", 0) <= 128, name
+    assert len(seen) == 6 * 3 * 3         # pairs of types, activations, sizes
