@@ -116,8 +116,8 @@ template <int BT> struct GroupTiles {
             base = -1;                       // (the turn in the registers is the last one)
         }
     }
-    // Group e of row tile `tile` < total, its first row and the end of its group.
-    __device__ __forceinline__ void find(const MatmulArgs& p, int tile, int& e, int& m0, int& end)
+    // Group e of row tile `tile` < total, its first row tile (of all), its rows [m0, end).
+    __device__ __forceinline__ void find(const MatmulArgs& p, int tile, int& e, int& first, int& m0, int& end)
     {
         if (base < 0)
             for (base = 0, before = 0;; base += 64) {
@@ -126,10 +126,10 @@ template <int BT> struct GroupTiles {
                 before += t;
             }
         const int at = __builtin_ctzll(__ballot(tile - before < upto));
-        const int l = __builtin_amdgcn_readlane(lo, at), h = __builtin_amdgcn_readlane(hi, at), u = __builtin_amdgcn_readlane(upto, at);
+        m0 = __builtin_amdgcn_readlane(lo, at);
+        end = __builtin_amdgcn_readlane(hi, at);
+        first = before + __builtin_amdgcn_readlane(upto, at) - (end - m0 + BT - 1) / BT;
         e = base + at;
-        m0 = l + (tile - before - (u - (h - l + BT - 1) / BT)) * BT;
-        end = h;
     }
 };
 
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(Matmu
     const int ntn = (p.N + BN - 1) / BN;
 
     // The place of this workgroup: neighbours in the order of launch go to different XCDs, so the ids are dealt out again such
-    // that an XCD walks over neighbouring tiles, eight row tiles by eight column tiles at a time.
+    // that an XCD walks over neighbouring tiles, column after column of eight row tiles, or of all of a group where those are fewer.
     int ntm = (p.M + BT - 1) / BT;
     std::conditional_t<GROUPED, GroupTiles<BT>, NoGroups> groups(p);
     if constexpr (GROUPED) ntm = groups.total;
@@ -247,11 +247,17 @@ __global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(Matmu
         const int each = total >> 3, more = total & 7, xcd = id & 7, at = id >> 3;
         id = xcd * each + min(xcd, more) + at;
     }
-    const int band = id / (8 * ntn), inband = id - band * 8 * ntn, height = min(8, ntm - band * 8);
+    int e = 0, m0 = 0, hi = p.M, high = ntm;     // the group, its first row and the row behind its last, its row tiles
+    if constexpr (GROUPED) {
+        int first;
+        groups.find(p, __builtin_amdgcn_readfirstlane(id / ntn), e, first, m0, hi);
+        id -= first * ntn;
+        high = (hi - m0 + BT - 1) / BT;
+    }
+    const int band = id / (8 * ntn), inband = id - band * 8 * ntn, height = min(8, high - band * 8);
     // (divisions are done in vector registers; what comes of these is the same in every lane and belongs in scalar ones)
     const int tn = __builtin_amdgcn_readfirstlane(inband / height), tm = __builtin_amdgcn_readfirstlane(band * 8 + inband - tn * height);
-    int e = 0, m0 = tm * BT, hi = p.M;
-    if constexpr (GROUPED) groups.find(p, tm, e, m0, hi);
+    m0 += tm * BT;
     const int n0 = tn * BN;
     const int rows = min(BT, hi - m0);
 
@@ -511,7 +517,9 @@ template <int AT, int YT, bool GROUPED> __global__ __launch_bounds__(512) void m
     if constexpr (GROUPED) {
         GroupTiles<16> groups(p);
         if (tm >= groups.total) return;
-        groups.find(p, tm, e, m0, hi);
+        int first;
+        groups.find(p, tm, e, first, m0, hi);
+        m0 += (tm - first) * 16;
     }
     const int rows = min(16, hi - m0), c = lane & 15, q = lane >> 4;
     const uint8_t* w = p.b + (GROUPED ? e * p.b_expert : 0) + min(n0 + c, p.N - 1) * p.b_row + q * 16;
