@@ -29,8 +29,9 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch_rows(const MatmulArgs
 // 64 x 64 tiles; 32 rows of that, four a unit: 11.6 against 11.6), and for products of up to 16 rows.  Else the tile whose estimate is
 // smallest: a fixed part, and per round of workgroups that are resident together a start and a time per slab, which is shorter in a last
 // round that leaves half of the places empty.  The constants, in microseconds, are fitted to 311 products of 1 to 16384 rows, 4 to 64
-// groups, 200 to 3200 columns and 256 to 4096 summed values in every pair of types; on these the choice costs 2.1 % more than the
-// fastest form each time, without the split 64 tile 3.2 %, without the 128 tile of eight waves 2.4 %.  (Groups: half a tile more each.)
+// groups, 200 to 3200 columns and 256 to 4096 summed values in every pair of types; there the choice costs 2.1 % more than the fastest form
+// each time, without the split 64 tile 3.2 %; on 199 of them, timed again, 1.7 %, without the widest 2.3 %, the deep one 2.7 %, the 64 or the 128
+// tile 6 %.  Groups: half a tile more each, and one each at least where they have rows (2.0 % on 140 of them, 2.5 % without the latter).
 enum Form { kRows, kTile64, kTile64Split, kTile128, kTile128Deep, kTile256 };
 struct TileTime { Form form; int size, places; double start, slab, slab_half_empty; };
 constexpr TileTime kTiles[] = {{kTile64, 64, 512, 1.5, 0.41, 0.20},
@@ -47,7 +48,7 @@ Form pick_form(const MatmulArgs& p, bool grouped, bool widest)
     double least = 0.0;
     for (const TileTime& t : kTiles) {
         if (t.form == kTile256 && !widest) continue;
-        const double rows = (double)ceil_div(p.M, t.size) + (grouped ? 0.5 * p.E : 0.0);
+        const double even = (double)ceil_div(p.M, t.size), rows = grouped ? std::max(even + 0.5 * p.E, (double)std::min(p.E, p.M)) : even;
         const double tiles = std::ceil(rows) * (double)ceil_div(p.N, t.size);
         const double full = std::floor(tiles / t.places), rest = tiles - full * t.places;
         const double last = rest == 0.0 ? 0.0 : rest <= 0.5 * t.places ? t.slab_half_empty : t.slab;
