@@ -535,6 +535,22 @@ def _params(t, n: int, what: str):
     return t
 
 
+def _scales(t, a, rows: int, what: str):
+    """Scales of the codes `a` in blocks of rows x 128."""
+    import torch
+    shape = tuple(a.shape[:-2]) + (-(-a.shape[-2] // rows), -(-a.shape[-1] // BLOCK))
+    if t is None or t.dtype != torch.float32 or t.device != a.device or tuple(t.shape) != shape or (t.stride(-1) != 1 and shape[-1] > 1):
+        raise ValueError(f"{what}: {list(shape)} 32-bit floats beside the codes, with a contiguous last dimension")
+    return t
+
+
+def _integers(t, like, what: str):
+    import torch
+    if t.dtype != torch.int32 or t.device != like.device or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous 32-bit integers beside the operands")
+    return t
+
+
 def empty_codes(*shape, device="cuda"):
     """A tensor for codes, its rows on 16 bytes."""
     import torch
@@ -573,6 +589,9 @@ def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dt
     (M, K), N = _rows(a, "a").shape, _rows(b, "b").shape[0]
     if b.shape[1] != K:
         raise ValueError(f"b has {b.shape[1]} columns, a has {K}")
+    if a.dtype != torch.float8_e4m3fn or b.dtype != a.dtype or b.device != a.device:
+        raise ValueError("a and b: codes on one GPU")
+    _scales(a_scale, a, 1, "a_scale"), _scales(b_scale, b, BLOCK, "b_scale")
     y = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=a.device)
     op = BlockMatmul(M, N, K, y_type=y.dtype, act=act, a_row=a.stride(0), b_row=b.stride(0), a_scale_row=a_scale.stride(0), b_scale_row=b_scale.stride(0))
     ws, n = _workspace(op, a)
@@ -586,14 +605,19 @@ def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, 
     import torch
     _rows(a, "a"), _rows(b, "b")
     E, N, K = b.shape
-    if a.shape[1] != K or a.dtype != b.dtype or offsets.dtype != torch.int32 or offsets.numel() != E + 1 or (index is not None and index.dtype != torch.int32):
-        raise ValueError("a [rows, K] and b [E, N, K] of one type, offsets [E + 1] and index in 32-bit integers")
+    if a.dim() != 2 or a.shape[1] != K or a.dtype != b.dtype or a.device != b.device or offsets.numel() != E + 1:
+        raise ValueError("a [rows, K] and b [E, N, K] of one type on one GPU, offsets [E + 1]")
+    _integers(offsets, a, "offsets")
+    if index is not None:
+        _integers(index, a, "index")
     M = a.shape[0] if index is None else index.numel()
     codes = a.dtype == torch.float8_e4m3fn
+    if codes:
+        _scales(a_scale, a, 1, "a_scale"), _scales(b_scale, b, BLOCK, "b_scale")
     y = torch.empty(M, N, dtype=dtype or (torch.bfloat16 if codes else a.dtype), device=a.device)
     op = GroupedMatmul(M, N, K, E, a_type=a.dtype, y_type=y.dtype, act=act, a_rows=a.shape[0], a_row=a.stride(0), b_row=b.stride(1), b_expert=b.stride(0),
                        a_scale_row=a_scale.stride(0) if codes else 0, b_scale_row=b_scale.stride(1) if codes else 0, b_scale_expert=b_scale.stride(0) if codes else 0)
     ws, n = _workspace(op, a)
-    op.forward(a.data_ptr(), _ptr(a_scale), _ptr(index), offsets.contiguous().data_ptr(), b.data_ptr(), _ptr(b_scale), _ptr(_params(bias, E * N, "bias")),
+    op.forward(a.data_ptr(), _ptr(a_scale if codes else None), _ptr(index), offsets.data_ptr(), b.data_ptr(), _ptr(b_scale if codes else None), _ptr(_params(bias, E * N, "bias")),
                y.data_ptr(), _ptr(ws), n, _stream(a))
     return y

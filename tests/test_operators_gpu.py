@@ -622,3 +622,27 @@ def test_rows_further_than_32_bits_reach():
     off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
     flipped = B.matmul_grouped_torch(a[:, :K], b[None], off, s, t[None], index=idx, dtype=torch.float32)
     assert torch.equal(flipped, want.flip(0))
+
+
+def test_torch_conveniences_refuse_scales_and_integers_that_do_not_fit():
+    q, s = B.quantize_blocks_torch(torch.randn(8, 300, device="cuda"))
+    w, t = B.quantize_blocks_torch(torch.randn(2, 200, 300, device="cuda"), 128)
+    off = torch.tensor([0, 4, 8], dtype=torch.int32, device="cuda")
+    assert s.shape == (8, 3) and t.shape == (2, 2, 3)
+    for bad in (s[:, :2], s[:7], s.double(), s.cpu(), s.t().contiguous().t(), None):
+        with pytest.raises(ValueError):
+            B.matmul_blocks_torch(q, bad, w[0], t[0])
+        with pytest.raises(ValueError):
+            B.matmul_grouped_torch(q, w, off, bad, t)
+    for bad in (t[:, :1], t[:1], t.half(), None):
+        with pytest.raises(ValueError):
+            B.matmul_grouped_torch(q, w, off, s, bad)
+    with pytest.raises(ValueError):
+        B.matmul_blocks_torch(q.float().half(), s, w[0].float().half(), t[0])
+    for bad in (off.cpu(), off.long(), off[:2], torch.stack([off, off], 1)[:, 0]):
+        with pytest.raises(ValueError):
+            B.matmul_grouped_torch(q, w, bad, s, t)
+    for bad in (off.cpu(), off.long(), torch.stack([off, off], 1)[:, 0]):
+        with pytest.raises(ValueError):
+            B.matmul_grouped_torch(q, w, off, s, t, index=bad)
+    assert B.matmul_grouped_torch(q, w, off, s, t, index=off[:2]).shape == (2, 200)
