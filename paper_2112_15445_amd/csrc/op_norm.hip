@@ -4,7 +4,7 @@
 //
 //   one launch   a workgroup holds whole groups of one sample in its registers, all positions of them: mean, then the squared
 //                deviations from it, then the result, with no second look at memory.  Taken where that fits: some groups of a
-//                sample (norm_resident: their lanes have to be powers of two) or the whole sample (norm_sample).
+//                sample (norm_resident: their lanes have to be powers of two; norm_sample: any, or the whole sample).
 //   two launches statistics of stretches of positions (each: mean and sum of squared deviations, put together pairwise, never as
 //                a difference of large sums), then the result, whose workgroups first put their sample's stretches together.
 //                x comes from the last-level cache the second time where it fits there (256 MB).
@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <numeric>
 
 namespace sc {
 namespace {
@@ -30,8 +31,8 @@ struct NormArgs {
     void* y;
     float* ys;
     float2* stats;                           // [N][G][stretches][parts] mean, sum of squared deviations
-    int N, S, C, G, Cg, NB;                  // (NB: blocks of 128 channels)
-    int seg, segs, parts;                    // channels of a statistics workgroup, segments of C, segments of one group (1: whole groups)
+    int N, S, C, G, Cg;
+    int seg, segs, parts;                    // channels of a workgroup of whole samples' parts, or of the statistics, segments of C, segments of one group (1: whole groups)
     int len, stretches;                      // positions of a stretch, stretches of a sample
     int rows;                                // positions of a workgroup of the second launch
     int once;                                // x and y do not stay in the last-level cache side by side: x passes it by
@@ -165,11 +166,12 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// One launch, groups of any size: a workgroup holds a whole sample, lanes side by side V neighbouring channels each.  Sums of channels go
+// One launch, groups of any size: a workgroup holds a whole sample or the groups of whole vectors of it (a.seg channels; codes: of whole
+// blocks), lanes side by side V neighbouring channels each.  Sums of channels go
 // through LDS and are put together by group (by_group), for the mean and then for the squared deviations from it.
 // ---------------------------------------------------------------------------------------------------------------------------
-// out[g] = the sum of value(g, row, channel of the group) over R rows and gc channels: by all T threads for one group, by a wave each
-// for a few, by sixteen lanes each for many.
+// out[g] = the sum of value(g, row, channel of the group) over R rows and gc channels: by several waves each for a few groups, by one
+// for some, by sixteen lanes each for many.
 template <int T, class F> __device__ __forceinline__ void by_group(int groups, int gc, int R, float* out, float* red, F value)
 {
     const float inv = 1.0f / (float)gc;
@@ -181,17 +183,21 @@ template <int T, class F> __device__ __forceinline__ void by_group(int groups, i
         }
         return s;
     };
-    if (groups == 1) {
-        const float s = sum64(part(0, threadIdx.x, T));
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    const int per = T / 64 / groups, wave = threadIdx.x >> 6;
+    if (per > 1) {
+        const int g = wave / per;
+        if (g < groups) {
+            const float s = sum64(part(g, threadIdx.x - g * per * 64, per * 64));
+            if ((threadIdx.x & 63) == 0) red[wave] = s;
+        }
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if ((int)threadIdx.x < groups) {
             float all = 0.0f;
-            for (int w = 0; w < T / 64; ++w) all += red[w];
-            out[0] = all;
+            for (int w = 0; w < per; ++w) all += red[threadIdx.x * per + w];
+            out[threadIdx.x] = all;
         }
     } else if (groups * 16 < T) {
-        for (int g = threadIdx.x >> 6; g < groups; g += T / 64) {
+        for (int g = wave; g < groups; g += T / 64) {
             const float s = sum64(part(g, threadIdx.x & 63, 64));
             if ((threadIdx.x & 63) == 0) out[g] = s;
         }
@@ -210,11 +216,11 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
     constexpr bool CODES = YT == SC_ELEM_E4M3;
     __shared__ float vals[T * V], red[T / 64];
     extern __shared__ float by[];                    // [2][G]
-    const int n = blockIdx.x;
-    const int tpr = CODES ? a.NB * L : (a.C + V - 1) / V, R = small_div(T, 1.0f / (float)tpr);
+    const int n = blockIdx.x, c0 = blockIdx.y * a.seg, C = min(a.seg, a.C - c0), G = C / a.Cg;      // its channels: C from c0 on
+    const int tpr = CODES ? (C + kQBlock - 1) / kQBlock * L : (C + V - 1) / V, R = small_div(T, 1.0f / (float)tpr);
     const int r = small_div(threadIdx.x, 1.0f / (float)tpr), v = threadIdx.x - r * tpr, c = v * V;
-    const int have = min(V, a.C - c), rows = r < R ? a.S : 0;
-    const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
+    const int have = min(V, C - c), rows = r < R ? a.S : 0;
+    const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c0 + c;
     v4i raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -222,15 +228,15 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
         if (r + u * R < rows && have > 0) raw[u] = have == V ? load_raw<XT>(x + (r + u * R) * a.x_row) : load_raw_part<XT>(x + (r + u * R) * a.x_row, have);
     }
     float gam[V], bet[V];
-    load_params<V>(gam, a.gamma, c, have, 1.0f);
-    load_params<V>(bet, a.beta, c, have, 0.0f);
+    load_params<V>(gam, a.gamma, c0 + c, have, 1.0f);
+    load_params<V>(bet, a.beta, c0 + c, have, 0.0f);
     const float cnt = (float)a.S * (float)a.Cg;
-    const int first = min(c, a.C - 1) / a.Cg, ends = (first + 1) * a.Cg - c;   // the group of a lane's first channel, its channels to come
+    const int first = min(c, C - 1) / a.Cg, ends = (first + 1) * a.Cg - c;   // the group of a lane's first channel, its channels to come
     auto each = [&](const float* t, auto take) {     // take(i, t of the group of channel c + i)
         int g = first, left = ends;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            take(i, t[min(g, a.G - 1)]);
+            take(i, t[min(g, G - 1)]);
             if (--left == 0) ++g, left = a.Cg;
         }
     };
@@ -250,7 +256,7 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
 #pragma unroll
         for (int i = 0; i < V; ++i) vals[threadIdx.x * V + i] = sum[i];
         __syncthreads();
-        by_group<T>(a.G, a.Cg, R, out, red, [&](int g, int rr, int cc) { return vals[rr * tpr * V + g * a.Cg + cc]; });
+        by_group<T>(G, a.Cg, R, out, red, [&](int g, int rr, int cc) { return vals[rr * tpr * V + g * a.Cg + cc]; });
     };
     together(by);
     forget();
@@ -264,9 +270,9 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[i] += (f[i] - mean[i]) * (f[i] - mean[i]);
         }
-    together(by + a.G);
+    together(by + G);
     forget();
-    each(by + a.G, [&](int i, float t) { gam[i] *= 1.0f / sqrtf(t / cnt + a.eps); });
+    each(by + G, [&](int i, float t) { gam[i] *= 1.0f / sqrtf(t / cnt + a.eps); });
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int pos = r + u * R;
@@ -274,14 +280,14 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
         float f[V];
         to_floats<XT>(raw[u], f);
         finish<ACT, V>(f, mean, gam, bet, have);
-        Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c;
+        Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c0 + c;
         if constexpr (CODES) {
             float amax = kAmaxFloor;
 #pragma unroll
             for (int i = 0; i < V; ++i) amax = fmaxf(amax, fabsf(f[i]));
             amax = max_block<L>(amax);
-            if (c < ((a.C + 15) & ~15)) store_codes<V>(y, f, kCodeMax / amax);
-            if (v % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + c / kQBlock] = amax / kCodeMax;
+            if (c < ((C + 15) & ~15)) store_codes<V>(y, f, kCodeMax / amax);
+            if (v % L == 0) a.ys[((int64_t)n * a.S + pos) * a.s_row + (c0 + c) / kQBlock] = amax / kCodeMax;
         } else {
             store_vec<YT, V>(y, f, have);
         }
@@ -488,7 +494,7 @@ bool pow2(int v) { return v > 0 && (v & (v - 1)) == 0; }
 
 struct NormShape {
     int T, U;                                // one launch (T = 0: two)
-    int TPR, LPG, dies;                      // ... of lanes in powers of two (TPR = 0: of whole samples)
+    int TPR, LPG, dies;                      // ... of lanes in powers of two (TPR = 0: of whole samples or parts of them: seg, segs)
     int seg, segs, parts, len, stretches;    // the statistics
     int wide, wides, rows, chunks;           // the result
     size_t bytes;
@@ -496,7 +502,7 @@ struct NormShape {
 
 // What a form takes, in microseconds: one launch 4.5 (of whole samples 5.5), two 11.5; then the larger of what memory takes at 4.5 TB/s
 // and, for one launch, what the fullest of 256 compute units takes at 5500 values a microsecond (three passes of 17 vector instructions in
-// all for each value).  Measured for estimated: 64 x 49 x 1040 (16 groups, f16) 15.7 for 14.8, 7 x 837 x 360 to codes 13.9 for 13.8,
+// all for each value).  Measured for estimated: 64 x 49 x 1040 (16 groups, f16) 15.7 for 14.8, in halves 12.7 for 10.1, 7 x 837 x 360 to codes 13.9 for 13.8,
 // 4 x 3000 x 416 17.5 for 18.2; 1 x 3136 x 64 (8 groups, f16) 11.3 in four workgroups, in two 15.8.
 double norm_time(const sc_group_norm_t* d, double base, double workgroups, double values, double reads)
 {
@@ -531,16 +537,32 @@ bool norm_resident(const sc_group_norm_t* d, NormShape* s, double* time)
     return any;
 }
 
-// One launch, a sample a workgroup: a sample in eight vectors a lane of 1024.
+// One launch, a sample a workgroup, or a part of one: the fewest groups that fill vectors (codes: blocks), times a power of two.  In
+// eight vectors a lane of 1024.  (64 x 49 x 1040, 16 groups, f16: whole samples 15.7 us, halves of them
+// 12.7; 6 x 427 x 1152, 16 groups, fp32: two launches 17.7, a workgroup a group 11.7.)
 bool norm_sample(const sc_group_norm_t* d, NormShape* s, double* time)
 {
     const int V = 16 / elem_bytes(d->x_type), L = kQBlock / V;
-    const int64_t tpr = d->y_type == SC_ELEM_E4M3 ? ceil_div(d->C, kQBlock) * L : ceil_div(d->C, V);
-    if (tpr > 1024 || d->G > 2048 || (int64_t)d->N * 1024 >= kMaxThreads) return false;
-    s->T = tpr <= 256 && 256 / tpr * 4 >= d->S ? 256 : 1024;
-    s->U = s->T / tpr * 4 >= d->S ? 4 : 8;
-    *time = norm_time(d, 5.5, d->N, (double)d->S * d->C, 1.0);
-    return s->T / tpr * s->U >= d->S;
+    const bool codes = d->y_type == SC_ELEM_E4M3;
+    bool any = false;
+    for (int64_t part = std::lcm<int64_t>(d->C / d->G, codes ? kQBlock : V);; part *= 2) {
+        part = std::min<int64_t>(part, d->C);
+        const int64_t tpr = codes ? ceil_div(part, kQBlock) * L : ceil_div(part, V), segs = ceil_div(d->C, part), bytes = part * elem_bytes(d->x_type);
+        if (tpr <= 1024 && part / (d->C / d->G) <= 2048 && segs <= 65535 && d->N * segs * 1024 < kMaxThreads) {
+            const int T = tpr <= 256 && 256 / tpr * 4 >= d->S ? 256 : 1024, U = T / tpr * 4 >= d->S ? 4 : 8;
+            // (parts that share lines read them twice)
+            const double t = norm_time(d, 5.5, (double)d->N * segs, (double)d->S * part, segs == 1 || bytes % 128 == 0 ? 1.0 : 1.0 + 128.0 / bytes);
+            if (T / tpr * U >= d->S && (!any || t <= *time)) {
+                any = true;
+                *time = t;
+                s->T = T;
+                s->U = U;
+                s->seg = (int)part;
+                s->segs = (int)segs;
+            }
+        }
+        if (part == d->C) return any;
+    }
 }
 
 NormShape norm_shape(const sc_group_norm_t* d)
@@ -599,8 +621,8 @@ sc_status_t check_norm(const sc_group_norm_t* d)
 template <int XT, int YT, int ACT> sc_status_t launch_norm(const sc_group_norm_t* d, const NormShape& s, const NormArgs& a, hipStream_t stream)
 {
     if (s.T && !s.TPR) {
-        const size_t lds = (size_t)d->G * 2 * sizeof(float);
-        const dim3 grid((unsigned)d->N);
+        const size_t lds = (size_t)(s.seg / a.Cg) * 2 * sizeof(float);
+        const dim3 grid((unsigned)d->N, (unsigned)s.segs);
         if (s.T == 256) norm_sample_kernel<XT, YT, ACT, 256, 4><<<grid, 256, lds, stream>>>(a);
         else if (s.U == 4) norm_sample_kernel<XT, YT, ACT, 1024, 4><<<grid, 1024, lds, stream>>>(a);
         else norm_sample_kernel<XT, YT, ACT, 1024, 8><<<grid, 1024, lds, stream>>>(a);
@@ -664,7 +686,7 @@ extern "C" sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const vo
     NormArgs a;
     a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.ys = y_scale;
     a.stats = static_cast<float2*>(workspace_dev);
-    a.N = d->N; a.S = d->S; a.C = d->C; a.G = d->G; a.Cg = d->C / d->G; a.NB = (int)ceil_div(d->C, kQBlock);
+    a.N = d->N; a.S = d->S; a.C = d->C; a.G = d->G; a.Cg = d->C / d->G;
     a.seg = shape.seg; a.segs = shape.segs; a.parts = shape.parts; a.len = shape.len; a.stretches = shape.stretches; a.rows = shape.rows;
     a.eps = d->eps;
     // (32 x 56x56 x 256 fp32, 206 MB: 47 us with the hint and 52 without; 39 MB of a quantiser's: 11.0 with and 10.4 without)

@@ -184,6 +184,15 @@ def test_group_norm(N, S, C, G, pad, lead, x_type, y_type):
     check_norm(x, G, gamma, beta, x_type, y_type, kind, (N, S, C, G, x_type, y_type, kind), pad=pad, lead=lead, y_pad=0 if pad == 0 else 5)
 
 
+@pytest.mark.parametrize("x_type,y_type", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "e4m3"), ("f16", "e4m3"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("N,S,C,G,pad,lead", [(2, 30, 416, 32, 0, 0), (3, 40, 1152, 16, 0, 0), (2, 9, 1040, 16, 3, 1), (1, 400, 768, 16, 0, 0), (2, 100, 1152, 12, 8, 0),
+                                              (1, 60, 156, 12, 0, 0), (1, 37, 1300, 100, 1, 0), (1, 200, 640, 2, 0, 0), (1, 2, 20000, 400, 0, 0)])
+def test_group_norm_of_parts_of_samples(N, S, C, G, pad, lead, x_type, y_type):
+    x, gamma, beta = norm_inputs(N, S, C, N + S + C)
+    kind = ("none", "relu", "silu")[(N + S + C + G) % 3]
+    check_norm(x, G, gamma, beta, x_type, y_type, kind, (N, S, C, G, x_type, y_type, kind), pad=pad, lead=lead, y_pad=0 if pad == 0 else 5)
+
+
 @pytest.mark.parametrize("kind", ["none", "relu", "silu"])
 @pytest.mark.parametrize("with_gamma,with_beta", [(False, False), (True, False), (False, True)])
 def test_group_norm_activations_and_missing_parameters(kind, with_gamma, with_beta):
