@@ -65,6 +65,15 @@ __device__ __forceinline__ void finish(float* f, const float* mean, const float*
     for (int i = 0; i < V; ++i) f[i] = i < have ? activate<ACT>((f[i] - mean[i]) * gam[i] + bet[i]) : 0.0f;
 }
 
+// The sample and part of this workgroup, of `parts` a sample.  dies: those of a sample go to one die, one after another, so that the pieces
+// of a line that they read and write meet in its cache (workgroups are dealt to the eight dies in turn).
+__device__ __forceinline__ void place(int parts, int dies, int& n, int& part)
+{
+    const int of = dies ? blockIdx.x >> 3 : blockIdx.x, at = of / parts;
+    n = dies ? at * 8 + (blockIdx.x & 7) : at;
+    part = of - at * parts;
+}
+
 // ---------------------------------------------------------------------------------------------------------------------------
 // One launch.  TPR lanes side by side cover the channels of a workgroup (16 bytes each, a power of two, LPG of them a group), the
 // others of the T lanes the positions; U positions a lane.  A sum over a group is a sum over lanes of a wave by shuffles and one over
@@ -75,10 +84,9 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
     constexpr int V = kVec<XT>, W = T / 64;
     __shared__ float red[2][W][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // dies: the workgroups of a sample go to one die, one after another, so that the pieces of a line that they read and write meet
-    // in its cache (workgroups are dealt to the eight dies in turn).
-    const int slabs = a.C / (TPR * V), of = dies ? blockIdx.x >> 3 : blockIdx.x, part = of / slabs;
-    const int n = dies ? part * 8 + (blockIdx.x & 7) : part, c0 = (of - part * slabs) * TPR * V;
+    int n, part;
+    place(a.C / (TPR * V), dies, n, part);
+    const int c0 = part * TPR * V;
     if (n >= a.N) return;
     const int col = threadIdx.x & (TPR - 1), r0 = threadIdx.x / TPR, R = T / TPR, c = c0 + col * V;
     const Elem<XT>* x = static_cast<const Elem<XT>*>(a.x) + n * a.x_sample + c;
@@ -210,13 +218,16 @@ template <int T, class F> __device__ __forceinline__ void by_group(int groups, i
     __syncthreads();
 }
 
-template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T, 4) void norm_sample_kernel(NormArgs a)
+template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T, 4) void norm_sample_kernel(NormArgs a, int dies)
 {
     constexpr int V = kVec<XT>, L = kQBlock / V;
     constexpr bool CODES = YT == SC_ELEM_E4M3;
     __shared__ float vals[T * V], red[T / 64];
     extern __shared__ float by[];                    // [2][G]
-    const int n = blockIdx.x, c0 = blockIdx.y * a.seg, C = min(a.seg, a.C - c0), G = C / a.Cg;      // its channels: C from c0 on
+    int n, part;
+    place(a.segs, dies, n, part);
+    if (n >= a.N) return;
+    const int c0 = part * a.seg, C = min(a.seg, a.C - c0), G = C / a.Cg;      // its channels: C from c0 on
     const int tpr = CODES ? (C + kQBlock - 1) / kQBlock * L : (C + V - 1) / V, R = small_div(T, 1.0f / (float)tpr);
     const int r = small_div(threadIdx.x, 1.0f / (float)tpr), v = threadIdx.x - r * tpr, c = v * V;
     const int have = min(V, C - c), rows = r < R ? a.S : 0;
@@ -494,37 +505,41 @@ bool pow2(int v) { return v > 0 && (v & (v - 1)) == 0; }
 
 struct NormShape {
     int T, U;                                // one launch (T = 0: two)
-    int TPR, LPG, dies;                      // ... of lanes in powers of two (TPR = 0: of whole samples or parts of them: seg, segs)
+    int dies, TPR, LPG;                      // ... of lanes in powers of two (TPR = 0: of whole samples or parts of them: seg, segs)
     int seg, segs, parts, len, stretches;    // the statistics
     int wide, wides, rows, chunks;           // the result
     size_t bytes;
 };
 
-// What a form takes, in microseconds: one launch 4.5 (of whole samples 5.5), two 11.5; then the larger of what memory takes at 4.5 TB/s
-// and, for one launch, what the fullest of 256 compute units takes at 5500 values a microsecond (three passes of 17 vector instructions in
-// all for each value).  Measured for estimated: 64 x 49 x 1040 (16 groups, f16) 15.7 for 14.8, in halves 12.7 for 10.1, 7 x 837 x 360 to codes 13.9 for 13.8,
-// 4 x 3000 x 416 17.5 for 18.2; 1 x 3136 x 64 (8 groups, f16) 11.3 in four workgroups, in two 15.8.
-double norm_time(const sc_group_norm_t* d, double base, double workgroups, double values, double reads)
+// What a form takes, in microseconds: one launch 4.5 (norm_sample 5.5), two 11.5; then the larger of what memory takes at 4.5 TB/s and, for one
+// launch of `parts` workgroups a sample, what the fullest of 256 compute units takes at 5500 values a microsecond (three passes of 17 vector
+// instructions in all for each value).  `reads`: how often a line comes from memory where the parts of a sample are on several dies; on one die
+// (`dies`) it comes once, but there are 32 compute units and an eighth of the bandwidth for each sample.
+// Measured for estimated: 7 x 837 x 360 to codes 13.9 for 13.8, 4 x 3000 x 416 17.0 for 18.2,
+// 1 x 3136 x 64 (8 groups, f16) 8.6 for 9.1 (four workgroups on several dies 11.3), 29 x 1883 x 64 (32 groups, bf16) 12.9 for 8.6 (15.3).
+double norm_time(const sc_group_norm_t* d, double base, double parts, double values, double reads, int* dies)
 {
-    const double total = (double)d->N * d->S * d->C;
-    return base + std::max(std::ceil(workgroups / kNumUnits) * values / 5500.0, total * (reads * elem_bytes(d->x_type) + elem_bytes(d->y_type)) / 4.5e6);
+    const double total = (double)d->N * d->S * d->C, x = elem_bytes(d->x_type), y = elem_bytes(d->y_type);
+    const double spread = std::max(std::ceil(d->N * parts / kNumUnits) * values / 5500.0, total * (reads * x + y) / 4.5e6);
+    const double held = std::max(std::ceil(std::ceil(d->N / 8.0) * parts / (kNumUnits / 8)) * values / 5500.0, total * (x + y) / (4.5e6 * std::min(d->N, 8) / 8));
+    *dies = parts > 1.0 && held <= spread;
+    return base + (*dies ? held : spread);
 }
 
 // One launch: groups of a power of two of 16-byte lanes, all positions of a workgroup's channels in 16 vectors a lane of 1024.  The
-// channels of a workgroup make a whole line of 128 bytes, or a part of one of at least 32 (codes: whole blocks of 128 channels): the
-// part of a line that the other workgroups need is read again, but where a die has all of them (`dies`).
+// channels of a workgroup make a whole line of 128 bytes, or a part of one (codes: whole blocks of 128 channels).
 bool norm_resident(const sc_group_norm_t* d, NormShape* s, double* time)
 {
     const int V = 16 / elem_bytes(d->x_type), Cg = d->C / d->G;
     const bool codes = d->y_type == SC_ELEM_E4M3;
     if (Cg % V || !pow2(Cg / V) || Cg / V > 64) return false;
-    const int LPG = Cg / V, line = codes ? kQBlock / V : 8, least = codes ? line : d->C == V ? 1 : 2;
-    const bool dies = d->N >= 16 || d->N == 8;
+    const int LPG = Cg / V, line = codes ? kQBlock / V : 8, least = codes ? line : 1;
     bool any = false;
     for (int TPR = LPG; TPR <= std::max(line, LPG) && d->C % (TPR * V) == 0; TPR *= 2) {
         const int64_t vectors = (int64_t)d->S * TPR;
         if (TPR < least || TPR % (codes ? line : 1) || vectors > 1024 * 16) continue;
-        const double t = norm_time(d, 4.5, (double)d->N * d->C / (TPR * V), (double)vectors * V, dies ? 1.0 : std::max(1.0, 8.0 / TPR));
+        int dies;
+        const double t = norm_time(d, 4.5, d->C / (TPR * V), (double)vectors * V, std::max(1.0, 8.0 / TPR), &dies);
         if (ceil_div(d->N, 8) * 8 * (d->C / (TPR * V)) * 1024 >= kMaxThreads || (any && t > *time)) continue;      // (level: the wider)
         any = true;
         *time = t;
@@ -548,15 +563,17 @@ bool norm_sample(const sc_group_norm_t* d, NormShape* s, double* time)
     for (int64_t part = std::lcm<int64_t>(d->C / d->G, codes ? kQBlock : V);; part *= 2) {
         part = std::min<int64_t>(part, d->C);
         const int64_t tpr = codes ? ceil_div(part, kQBlock) * L : ceil_div(part, V), segs = ceil_div(d->C, part), bytes = part * elem_bytes(d->x_type);
-        if (tpr <= 1024 && part / (d->C / d->G) <= 2048 && segs <= 65535 && d->N * segs * 1024 < kMaxThreads) {
+        if (tpr <= 1024 && part / (d->C / d->G) <= 2048 && ceil_div(d->N, 8) * 8 * segs * 1024 < kMaxThreads) {
             const int T = tpr <= 256 && 256 / tpr * 4 >= d->S ? 256 : 1024, U = T / tpr * 4 >= d->S ? 4 : 8;
             // (parts that share lines read them twice)
-            const double t = norm_time(d, 5.5, (double)d->N * segs, (double)d->S * part, segs == 1 || bytes % 128 == 0 ? 1.0 : 1.0 + 128.0 / bytes);
+            int dies;
+            const double t = norm_time(d, 5.5, (double)segs, (double)d->S * part, segs == 1 || bytes % 128 == 0 ? 1.0 : 1.0 + 128.0 / bytes, &dies);
             if (T / tpr * U >= d->S && (!any || t <= *time)) {
                 any = true;
                 *time = t;
                 s->T = T;
                 s->U = U;
+                s->dies = dies;
                 s->seg = (int)part;
                 s->segs = (int)segs;
             }
@@ -568,8 +585,8 @@ bool norm_sample(const sc_group_norm_t* d, NormShape* s, double* time)
 NormShape norm_shape(const sc_group_norm_t* d)
 {
     if (d->N == 0 || d->S == 0) return {};
-    double best = norm_time(d, 11.5, 0.0, 0.0, 2.0), time = 0.0;
     NormShape one{}, resident{}, sample{};
+    double best = norm_time(d, 11.5, 0.0, 0.0, 2.0, &one.dies), time = 0.0;
     if (norm_resident(d, &resident, &time) && time < best) one = resident, best = time;
     if (norm_sample(d, &sample, &time) && time < best) one = sample;
     if (one.T) return one;
@@ -620,16 +637,17 @@ sc_status_t check_norm(const sc_group_norm_t* d)
 
 template <int XT, int YT, int ACT> sc_status_t launch_norm(const sc_group_norm_t* d, const NormShape& s, const NormArgs& a, hipStream_t stream)
 {
+    const int64_t samples = s.dies ? ceil_div(d->N, 8) * 8 : (int64_t)d->N;
     if (s.T && !s.TPR) {
         const size_t lds = (size_t)(s.seg / a.Cg) * 2 * sizeof(float);
-        const dim3 grid((unsigned)d->N, (unsigned)s.segs);
-        if (s.T == 256) norm_sample_kernel<XT, YT, ACT, 256, 4><<<grid, 256, lds, stream>>>(a);
-        else if (s.U == 4) norm_sample_kernel<XT, YT, ACT, 1024, 4><<<grid, 1024, lds, stream>>>(a);
-        else norm_sample_kernel<XT, YT, ACT, 1024, 8><<<grid, 1024, lds, stream>>>(a);
+        const dim3 grid((unsigned)(samples * s.segs));
+        if (s.T == 256) norm_sample_kernel<XT, YT, ACT, 256, 4><<<grid, 256, lds, stream>>>(a, s.dies);
+        else if (s.U == 4) norm_sample_kernel<XT, YT, ACT, 1024, 4><<<grid, 1024, lds, stream>>>(a, s.dies);
+        else norm_sample_kernel<XT, YT, ACT, 1024, 8><<<grid, 1024, lds, stream>>>(a, s.dies);
         return launched();
     }
     if (s.T) {
-        const dim3 grid((unsigned)((s.dies ? ceil_div(d->N, 8) * 8 : (int64_t)d->N) * (d->C / (s.TPR * kVec<XT>))));
+        const dim3 grid((unsigned)(samples * (d->C / (s.TPR * kVec<XT>))));
         if (s.T == 256) norm_resident_kernel<XT, YT, ACT, 256, 4><<<grid, 256, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
         else if (s.U == 4) norm_resident_kernel<XT, YT, ACT, 512, 4><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
         else if (s.T == 512) norm_resident_kernel<XT, YT, ACT, 512, 16><<<grid, 512, 0, stream>>>(a, s.TPR, s.LPG, s.dies);
