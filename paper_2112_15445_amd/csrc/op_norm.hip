@@ -9,8 +9,8 @@
 //                a difference of large sums), then the result, whose workgroups first put their sample's stretches together.
 //                x comes from the last-level cache the second time where it fits there (256 MB).
 //
-// Measured: 32 x 56x56 x 256 fp32 (206 MB) 47 us, 4.3 TB/s, where a copy of as much takes 40; 7x7 x 2048 f16 4.5 us on the GPU, little more than a
-// launch; 7 x 27x31 x 360 bf16 to codes (groups of 12) in two launches 6.4 + 8.3 us, each a launch, one or two trips to memory and its arithmetic.
+// Measured: 32 x 56x56 x 256 fp32 (206 MB) 45-47 us, 4.4 TB/s, where a copy of as much takes 40; 7x7 x 2048 f16 4.5 us on the GPU, little more than a
+// launch; 7 x 27x31 x 360 bf16 to codes (groups of 12) in two launches 6.4 + 8.2 us, each a launch, one or two trips to memory and its arithmetic.
 #include "op_common.h"
 
 #include <algorithm>
@@ -601,7 +601,8 @@ NormShape norm_shape(const sc_group_norm_t* d)
         s.parts = (int)ceil_div(Cg, most);
         s.segs = d->G * s.parts;
     }
-    // Four workgroups a compute unit for both launches, no stretch under eight vectors a lane.
+    // Four workgroups a compute unit for the first launch, eight for the second, no stretch under eight vectors a lane, no fewer than four a lane in the
+    // second (7 x 837 x 360 to codes: 13.9 us; five vectors a lane in the first 14.3, twelve 14.7; two in the second 14.4, eight 15.5).
     const int R = std::max<int>(1, kThreads / (int)ceil_div(std::min(s.seg, d->C), V));
     const int64_t want = std::max<int64_t>(1, 1024 / ((int64_t)d->N * s.segs));
     s.stretches = (int)std::min<int64_t>({want, kMaxStretches, kParts / s.parts, ceil_div(d->S, 8 * R)});
