@@ -563,7 +563,7 @@ def group_norm_torch(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, a
     _rows(x, "x")
     N, S, C = x.shape
     y = empty_codes(N * S, C, device=x.device) if codes else torch.empty((N, S, C), dtype=x.dtype, device=x.device)
-    scale = torch.empty(N * S, -(-C // BLOCK), device=x.device) if codes else None
+    scale = torch.empty(N * S, -(-C // BLOCK), dtype=torch.float32, device=x.device) if codes else None
     op = GroupNorm(N, S, C, groups, eps=eps, act=act, x_type=x.dtype, y_type=y.dtype, x_strides=x.stride()[:2])
     ws, n = _workspace(op, x)
     op.forward(x.data_ptr(), _ptr(_params(gamma, C, "gamma")), _ptr(_params(beta, C, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n, _stream(x))
@@ -576,7 +576,7 @@ def quantize_blocks_torch(x, rows: int = 1):
     _rows(x, "x")
     lead, (M, K) = x.shape[:-2], x.shape[-2:]
     q = empty_codes(*lead, M, K, device=x.device)
-    scale = torch.empty(*lead, -(-M // rows), -(-K // BLOCK), device=x.device)
+    scale = torch.empty(*lead, -(-M // rows), -(-K // BLOCK), dtype=torch.float32, device=x.device)
     op = BlockQuantizer(M, K, rows=rows, x_type=x.dtype, x_row=x.stride(-2), q_row=q.stride(-2))
     for i in np.ndindex(*lead):
         op.forward(x[i].data_ptr(), q[i].data_ptr(), scale[i].data_ptr(), _stream(x))
