@@ -586,7 +586,7 @@ sc_status_t sparse_conv_matmul_grouped_workspace_size(const sc_matmul_grouped_t*
 
 /*   a, b device, as for sparse_conv_matmul_blocks     a_scale, b_scale E4M3 only
  *   index device i32 [M] or NULL     offsets device i32 [E + 1]     bias device f32 [E][N] or NULL
- * Errors: as sparse_conv_matmul_blocks. */
+ * Errors: as sparse_conv_matmul_blocks; SC_ERR_RANGE also for experts 2^48 elements or more apart. */
 sc_status_t sparse_conv_matmul_grouped(const sc_matmul_grouped_t* d, const void* a, const float* a_scale,
                                        const int32_t* index, const int32_t* offsets, const void* b, const float* b_scale,
                                        const float* bias, void* y, void* workspace_dev, size_t workspace_bytes,

@@ -78,6 +78,7 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch(const MatmulArgs& p, 
 
 constexpr int64_t kMaxRowBytes = (int64_t)1 << 22;     // (256 rows of a tile are addressed with 32 bits)
 constexpr int kMaxRows = 1 << 30;
+constexpr int64_t kMaxExpert = (int64_t)1 << 48;       // (of elements: 4096 experts are addressed with 64 bits)
 
 sc_status_t check_blocks(const sc_matmul_blocks_t* d)
 {
@@ -98,10 +99,11 @@ sc_status_t check_grouped(const sc_matmul_grouped_t* d)
     if (d->a_type != SC_ELEM_F16 && d->a_type != SC_ELEM_BF16 && !codes) return SC_ERR_UNSUPPORTED;
     if (!is_wide(d->y_type) || (!codes && d->y_type != d->a_type && d->y_type != SC_ELEM_F32)) return SC_ERR_UNSUPPORTED;
     const int64_t KB = ceil_div(d->K, kQBlock), e = elem_bytes(d->a_type);
+    // (distances are compared as they are: multiplied by the element's size or by rows, a large one could pass for a small one)
+    if (d->M > kMaxRows || d->a_row >= kMaxRowBytes / e || d->b_row >= kMaxRowBytes / e || (d->E > 1 && d->b_expert >= kMaxExpert)) return SC_ERR_RANGE;
     if (d->b_expert < (d->N - 1) * d->b_row + d->K && d->E > 1) return SC_ERR_SHAPE;
     if (codes && (d->a_scale_row < KB || d->b_scale_row < KB || (d->E > 1 && d->b_scale_expert < ceil_div(d->N, kQBlock) * KB))) return SC_ERR_SHAPE;
-    if (d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || d->a_row * e % 16 || d->b_row * e % 16 || d->b_expert * e % 16) return SC_ERR_UNSUPPORTED;
-    if (d->M > kMaxRows || d->a_row * e >= kMaxRowBytes || d->b_row * e >= kMaxRowBytes) return SC_ERR_RANGE;
+    if (d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || d->a_row % (16 / e) || d->b_row % (16 / e) || d->b_expert % (16 / e)) return SC_ERR_UNSUPPORTED;
     return SC_OK;
 }
 
@@ -168,7 +170,7 @@ extern "C" sc_status_t sparse_conv_matmul_grouped(const sc_matmul_grouped_t* d, 
     p.a = static_cast<const uint8_t*>(a); p.b = static_cast<const uint8_t*>(b); p.as = a_scale; p.bs = b_scale; p.bias = bias;
     p.index = index; p.offsets = offsets; p.y = y;
     p.M = d->M; p.N = d->N; p.E = d->E; p.a_rows = d->a_rows; p.kbytes = d->K * e;
-    p.a_row = d->a_row * e; p.b_row = d->b_row * e; p.b_expert = d->b_expert * e; p.y_row = d->y_row;
+    p.a_row = d->a_row * e; p.b_row = d->b_row * e; p.b_expert = d->E > 1 ? d->b_expert * e : 0; p.y_row = d->y_row;
     p.as_row = d->a_scale_row; p.bs_row = d->b_scale_row; p.bs_expert = d->b_scale_expert; p.act = d->act;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool f32 = d->y_type == SC_ELEM_F32;

@@ -1,0 +1,25 @@
+"""Sizes and distances at the ends of their types: the operators refuse what they could not address.  No call here gets as far as a launch."""
+import pytest
+
+from paper_2112_15445_amd import binding as B
+
+SHAPE, UNSUPPORTED, RANGE, WORKSPACE = 2, 4, 5, 7
+P = 0x10000                          # an address that is never read
+
+
+def refused(status, op, *args):
+    with pytest.raises(B.SparseConvError) as e:
+        op.forward(*args)
+    assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("a_type", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("far", [1 << 22, 1 << 31, 1 << 61, 1 << 62])
+def test_grouped_distances_are_compared_before_they_are_multiplied(a_type, far):
+    """1 << 62 values of two bytes are 0 bytes modulo 2^64, 1 << 61 of 8 rows the same: neither may pass for a small distance."""
+    args = [P, P, 0, P, P, P, 0, P, P, 1 << 30]
+    refused(RANGE, B.GroupedMatmul(8, 16, 32, 2, a_type=a_type, a_row=far), *args)
+    refused(RANGE, B.GroupedMatmul(8, 16, 32, 2, a_type=a_type, b_row=far, b_expert=1 << 40), *args)
+    refused(RANGE, B.GroupedMatmul(8, 9, 32, 1, a_type=a_type, b_row=far, b_expert=0), *args)
+    if far > 1 << 59:
+        refused(RANGE, B.GroupedMatmul(8, 16, 32, 2, a_type=a_type, b_expert=far), *args)
