@@ -506,7 +506,7 @@ sc_status_t sparse_conv_group_norm_workspace_size(const sc_group_norm_t* d, size
  *           the next multiple of 16 are written with zero codes).  y may be x, with x's type and distances.
  *   y_scale device f32 [N S][scale_row], E4M3 only
  * Errors: SC_ERR_NULL, SC_ERR_SHAPE (sizes, G not dividing C, distances), SC_ERR_UNSUPPORTED (types,
- * activation, eps, alignment), SC_ERR_RANGE (S * C or N * S >= 2^31, C / G >= 2^20, more
+ * activation, eps, alignment), SC_ERR_RANGE (S * C or N * S >= 2^31, S > 2^30, C / G >= 2^20, more
  * workgroups than a launch has), SC_ERR_WORKSPACE, SC_ERR_HIP. */
 sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const void* x, const float* gamma, const float* beta,
                                    void* y, float* y_scale, void* workspace_dev, size_t workspace_bytes, void* stream);

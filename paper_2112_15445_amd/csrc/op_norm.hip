@@ -625,6 +625,7 @@ sc_status_t check_norm(const sc_group_norm_t* d)
     if (!is_wide(d->x_type) || (d->y_type != d->x_type && d->y_type != SC_ELEM_E4M3)) return SC_ERR_UNSUPPORTED;
     if (d->act < SC_ACT_NONE || d->act > SC_ACT_SILU || !(d->eps >= 0.0f) || d->eps > 3e38f) return SC_ERR_UNSUPPORTED;
     if ((int64_t)d->S * d->C >= (int64_t)1 << 31 || (int64_t)d->N * d->S >= (int64_t)1 << 31) return SC_ERR_RANGE;
+    if (d->S > 1 << 30) return SC_ERR_RANGE;                 // (a workgroup looks up to its own number of positions beyond its last one, in 32 bits)
     if (d->C / d->G >= 1 << 20) return SC_ERR_RANGE;         // (the parts of a group: kParts of 1024 channels or more)
     if (d->x_sample < 0 || d->x_row < 0) return SC_ERR_SHAPE;
     if (d->y_row < d->C) return SC_ERR_SHAPE;

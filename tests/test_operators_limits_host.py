@@ -23,3 +23,16 @@ def test_grouped_distances_are_compared_before_they_are_multiplied(a_type, far):
     refused(RANGE, B.GroupedMatmul(8, 9, 32, 1, a_type=a_type, b_row=far, b_expert=0), *args)
     if far > 1 << 59:
         refused(RANGE, B.GroupedMatmul(8, 16, 32, 2, a_type=a_type, b_expert=far), *args)
+
+
+@pytest.mark.parametrize("S", [(1 << 30) + 1, (1 << 31) - (1 << 20), (1 << 31) - 1])
+@pytest.mark.parametrize("x_type", ["f32", "f16", "bf16"])
+def test_group_norm_refuses_positions_that_its_counters_pass(S, x_type):
+    """Positions are counted in 32 bits, and a workgroup looks some beyond its own before it stops."""
+    for y_type in (x_type, "e4m3"):
+        op = B.GroupNorm(1, S, 1, 1, x_type=x_type, y_type=y_type)
+        refused(RANGE, op, P, P, P, P, P, P, 1 << 30)
+        with pytest.raises(B.SparseConvError) as e:
+            op.workspace_size()
+        assert e.value.status == RANGE
+    assert B.GroupNorm(1, 1 << 30, 1, 1, x_type=x_type).workspace_size() > 0
