@@ -629,7 +629,7 @@ sc_status_t check_norm(const sc_group_norm_t* d)
     if (d->C / d->G >= 1 << 20) return SC_ERR_RANGE;         // (the parts of a group: kParts of 1024 channels or more)
     if (d->x_sample < 0 || d->x_row < 0) return SC_ERR_SHAPE;
     if (d->y_row < d->C) return SC_ERR_SHAPE;
-    if (d->N > 1 && d->S > 0 && d->y_sample < (d->S - 1) * d->y_row + d->C) return SC_ERR_SHAPE;
+    if (d->N > 1 && d->S > 0 && d->y_sample < (__int128)(d->S - 1) * d->y_row + d->C) return SC_ERR_SHAPE;      // (the product may pass 64 bits)
     if (d->y_type == SC_ELEM_E4M3) {
         if (d->scale_row < ceil_div(d->C, kQBlock)) return SC_ERR_SHAPE;
         if (d->y_row % 16 || d->y_sample % 16) return SC_ERR_UNSUPPORTED;

@@ -36,3 +36,9 @@ def test_group_norm_refuses_positions_that_its_counters_pass(S, x_type):
             op.workspace_size()
         assert e.value.status == RANGE
     assert B.GroupNorm(1, 1 << 30, 1, 1, x_type=x_type).workspace_size() > 0
+
+
+def test_group_norm_compares_samples_without_overflow():
+    """(S - 1) y_row + C beyond 64 bits is no distance that samples could have."""
+    refused(SHAPE, B.GroupNorm(2, 5, 32, 4, y_strides=(1 << 40, 1 << 62)), P, P, P, P, 0, P, 1 << 20)
+    refused(SHAPE, B.GroupNorm(2, 3, 32, 4, y_strides=(1 << 40, 1 << 62)), P, P, P, P, 0, P, 1 << 20)
