@@ -529,7 +529,7 @@ typedef struct {
 /*   x device, element-aligned      q device, 16-byte aligned; the codes between column K and the next multiple
  *   of 16 are written as zeros     scale device f32 [ceil(M / rows)][scale_row]
  * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (rows, types, alignment), SC_ERR_RANGE (2^27 or more blocks of
- * one row, 2^22 or more of 128), SC_ERR_HIP. */
+ * one row, 2^22 or more of 128, K > 2^31 - 256), SC_ERR_HIP. */
 sc_status_t sparse_conv_quantize_blocks(const sc_quantize_blocks_t* d, const void* x, void* q, float* scale, void* stream);
 
 /* Product of an M x K matrix of activations and an N x K matrix of weights in blocks:

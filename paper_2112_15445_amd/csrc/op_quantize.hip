@@ -106,6 +106,7 @@ extern "C" sc_status_t sparse_conv_quantize_blocks(const sc_quantize_blocks_t* d
     if (!d) return SC_ERR_NULL;
     if (d->M < 0 || d->K <= 0 || d->x_row < 0 || d->q_row < d->K || d->scale_row < ceil_div(d->K, kQBlock)) return SC_ERR_SHAPE;
     if ((d->rows != 1 && d->rows != kQBlock) || !is_wide(d->x_type) || d->q_row % 16) return SC_ERR_UNSUPPORTED;
+    if (d->K > INT32_MAX - 255) return SC_ERR_RANGE;         // (columns are counted to the end of the last block, in 32 bits)
     if (ceil_div(d->M, d->rows) * ceil_div(d->K, kQBlock) >= (int64_t)1 << (d->rows == 1 ? 27 : 22)) return SC_ERR_RANGE;   // threads of a launch
     if (d->M == 0) return SC_OK;
     if (!x || !q || !scale) return SC_ERR_NULL;

@@ -42,3 +42,11 @@ def test_group_norm_compares_samples_without_overflow():
     """(S - 1) y_row + C beyond 64 bits is no distance that samples could have."""
     refused(SHAPE, B.GroupNorm(2, 5, 32, 4, y_strides=(1 << 40, 1 << 62)), P, P, P, P, 0, P, 1 << 20)
     refused(SHAPE, B.GroupNorm(2, 3, 32, 4, y_strides=(1 << 40, 1 << 62)), P, P, P, P, 0, P, 1 << 20)
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("K", [(1 << 31) - 255, (1 << 31) - 15, (1 << 31) - 1])
+def test_the_quantiser_refuses_columns_that_its_counters_pass(K, rows):
+    """Columns are counted in 32 bits, up to the end of the last block and to the next multiple of 16."""
+    refused(RANGE, B.BlockQuantizer(1, K, rows=rows), P, P, P)
+    B.BlockQuantizer(0, (1 << 31) - 256, rows=rows).forward(0, 0, 0)
