@@ -586,7 +586,9 @@ def quantize_blocks_torch(x, rows: int = 1):
 def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dtype=None):
     """act(a b^T + bias) of codes a [M, K] with scales of 1 x 128 and b [N, K] with scales of 128 x 128 blocks."""
     import torch
-    (M, K), N = _rows(a, "a").shape, _rows(b, "b").shape[0]
+    if _rows(a, "a").dim() != 2 or _rows(b, "b").dim() != 2:
+        raise ValueError(f"a and b: matrices, not {list(a.shape)} and {list(b.shape)} (a stack of weights goes to matmul_grouped_torch)")
+    (M, K), N = a.shape, b.shape[0]
     if b.shape[1] != K:
         raise ValueError(f"b has {b.shape[1]} columns, a has {K}")
     if a.dtype != torch.float8_e4m3fn or b.dtype != a.dtype or b.device != a.device:

@@ -55,3 +55,15 @@ def test_scales_are_32_bit_floats_whatever_the_default_type(calls, default):
     assert [s.dtype for s in scales] == [torch.float32] * 3
     assert [tuple(s.shape) for s in scales] == [(10, 3), (9, 3), (3, 2, 3)]
     assert len(calls) == 5
+
+
+def test_a_stack_of_weights_is_no_matrix(calls):
+    """Square experts [E, K, K] with the scales that belong to them look like E columns of K values."""
+    a, s = codes(6, 256), tensor(6, 2, dtype=torch.float32)
+    for E, N in ((4, 256), (2, 256), (256, 256)):
+        with pytest.raises(ValueError):
+            B.matmul_blocks_torch(a, s, codes(E, N, 256), tensor(E, 2, 2, dtype=torch.float32))
+    with pytest.raises(ValueError):
+        B.matmul_blocks_torch(codes(2, 6, 256), tensor(2, 6, 2, dtype=torch.float32), codes(256, 256), tensor(2, 2, dtype=torch.float32))
+    assert not calls
+    assert B.matmul_blocks_torch(a, s, codes(40, 256), tensor(1, 2, dtype=torch.float32)).shape == (6, 40)
