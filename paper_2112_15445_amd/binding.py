@@ -487,7 +487,7 @@ def torch_out_dtype(dtype: int):
 
 
 def forward_torch(plan: Plan, x, y=None, workspace=None):
-    """Run sparse_conv_forward on torch CUDA tensors on torch's current stream."""
+    """Run sparse_conv_forward on torch CUDA tensors, on their device and torch's current stream there."""
     import torch
     assert x.is_cuda and x.is_contiguous()
     N = x.shape[0]
@@ -497,19 +497,22 @@ def forward_torch(plan: Plan, x, y=None, workspace=None):
     need = plan.workspace_size(N)
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    stream = torch.cuda.current_stream(x.device).cuda_stream
-    plan.forward(x.data_ptr(), y.data_ptr(), N,
-                 workspace.data_ptr() if workspace is not None else 0,
-                 workspace.numel() * workspace.element_size() if workspace is not None else 0, stream)
+    with torch.cuda.device(x.device):
+        plan.forward(x.data_ptr(), y.data_ptr(), N,
+                     workspace.data_ptr() if workspace is not None else 0,
+                     workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                     torch.cuda.current_stream(x.device).cuda_stream)
     return y
 
 
-# ... and of the operators of channels-last blocks: tensors in, tensors out, on torch's current stream.  Rows may lie further apart than
+# ... and of the operators of channels-last blocks: tensors in, tensors out, on their device and torch's current stream there.  Rows may lie further apart than
 # their length; the last dimension is contiguous.
 
-def _stream(t) -> int:
+def _call(op, like, *args):
+    """op.forward on the device where `like` lies, on torch's current stream there, whatever device is the current one."""
     import torch
-    return torch.cuda.current_stream(t.device).cuda_stream
+    with torch.cuda.device(like.device):
+        op.forward(*args, torch.cuda.current_stream(like.device).cuda_stream)
 
 
 def _workspace(op, like):
@@ -566,7 +569,7 @@ def group_norm_torch(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, a
     scale = torch.empty(N * S, -(-C // BLOCK), dtype=torch.float32, device=x.device) if codes else None
     op = GroupNorm(N, S, C, groups, eps=eps, act=act, x_type=x.dtype, y_type=y.dtype, x_strides=x.stride()[:2])
     ws, n = _workspace(op, x)
-    op.forward(x.data_ptr(), _ptr(_params(gamma, C, "gamma")), _ptr(_params(beta, C, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n, _stream(x))
+    _call(op, x, x.data_ptr(), _ptr(_params(gamma, C, "gamma")), _ptr(_params(beta, C, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n)
     return (y, scale) if codes else y
 
 
@@ -579,7 +582,7 @@ def quantize_blocks_torch(x, rows: int = 1):
     scale = torch.empty(*lead, -(-M // rows), -(-K // BLOCK), dtype=torch.float32, device=x.device)
     op = BlockQuantizer(M, K, rows=rows, x_type=x.dtype, x_row=x.stride(-2), q_row=q.stride(-2))
     for i in np.ndindex(*lead):
-        op.forward(x[i].data_ptr(), q[i].data_ptr(), scale[i].data_ptr(), _stream(x))
+        _call(op, x, x[i].data_ptr(), q[i].data_ptr(), scale[i].data_ptr())
     return q, scale
 
 
@@ -597,7 +600,7 @@ def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dt
     y = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=a.device)
     op = BlockMatmul(M, N, K, y_type=y.dtype, act=act, a_row=a.stride(0), b_row=b.stride(0), a_scale_row=a_scale.stride(0), b_scale_row=b_scale.stride(0))
     ws, n = _workspace(op, a)
-    op.forward(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(_params(bias, N, "bias")), y.data_ptr(), _ptr(ws), n, _stream(a))
+    _call(op, a, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(_params(bias, N, "bias")), y.data_ptr(), _ptr(ws), n)
     return y
 
 
@@ -620,6 +623,6 @@ def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, 
     op = GroupedMatmul(M, N, K, E, a_type=a.dtype, y_type=y.dtype, act=act, a_rows=a.shape[0], a_row=a.stride(0), b_row=b.stride(1), b_expert=b.stride(0),
                        a_scale_row=a_scale.stride(0) if codes else 0, b_scale_row=b_scale.stride(1) if codes else 0, b_scale_expert=b_scale.stride(0) if codes else 0)
     ws, n = _workspace(op, a)
-    op.forward(a.data_ptr(), _ptr(a_scale if codes else None), _ptr(index), offsets.data_ptr(), b.data_ptr(), _ptr(b_scale if codes else None), _ptr(_params(bias, E * N, "bias")),
-               y.data_ptr(), _ptr(ws), n, _stream(a))
+    _call(op, a, a.data_ptr(), _ptr(a_scale if codes else None), _ptr(index), offsets.data_ptr(), b.data_ptr(), _ptr(b_scale if codes else None),
+          _ptr(_params(bias, E * N, "bias")), y.data_ptr(), _ptr(ws), n)
     return y

@@ -67,3 +67,38 @@ def test_a_stack_of_weights_is_no_matrix(calls):
         B.matmul_blocks_torch(codes(2, 6, 256), tensor(2, 6, 2, dtype=torch.float32), codes(256, 256), tensor(2, 2, dtype=torch.float32))
     assert not calls
     assert B.matmul_blocks_torch(a, s, codes(40, 256), tensor(1, 2, dtype=torch.float32)).shape == (6, 40)
+
+
+def test_calls_are_made_on_the_device_of_the_tensors(calls):
+    """cuda:0 is current and the tensors lie on cuda:1: the call is made with cuda:1 current and on its stream, and cuda:0 is current again."""
+    on = "cuda:1"
+    q, s = B.group_norm_torch(tensor(2, 5, 256, device=on), 8, tensor(256, dtype=torch.float32, device=on), tensor(256, dtype=torch.float32, device=on), codes=True)
+    B.group_norm_torch(tensor(1, 3000, 48, device=on), 3)                      # (takes a workspace)
+    w, t = B.quantize_blocks_torch(tensor(2, 200, 256, device=on), 128)
+    B.matmul_blocks_torch(q, s, w[0], t[0], bias=tensor(200, dtype=torch.float32, device=on))
+    B.matmul_grouped_torch(q, w, tensor(3, dtype=torch.int32, device=on), s, t)
+    assert [c[2] for c in calls] == [1] * 6 and [c[1][-1] for c in calls] == [101] * 6
+    assert q.device == s.device == w.device == t.device == torch.device(on)
+    assert torch.cuda.current_stream().cuda_stream == 100
+
+
+def test_convolutions_are_made_on_the_device_of_the_tensors(calls):
+    class Plan:
+        dtype = B.SC_F32
+
+        class layer:
+            D = 4
+
+        def info(self):
+            class I:
+                P = Q = 3
+            return I
+
+        def workspace_size(self, n):
+            return 64
+
+        def forward(self, *a):
+            calls.append((self, a, torch.cuda.current_stream().cuda_stream - 100))
+
+    y = B.forward_torch(Plan(), tensor(2, 3, 5, 5, dtype=torch.float32, device="cuda:1"))
+    assert y.device == torch.device("cuda:1") and calls[0][2] == 1 and calls[0][1][-1] == 101
