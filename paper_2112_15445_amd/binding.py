@@ -531,10 +531,10 @@ def _rows(t, what: str):
     return t
 
 
-def _params(t, n: int, what: str):
+def _params(t, n: int, like, what: str):
     import torch
-    if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
-        raise ValueError(f"{what}: {n} contiguous 32-bit floats on the GPU")
+    if t is not None and not (t.device == like.device and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
+        raise ValueError(f"{what}: {n} contiguous 32-bit floats on the GPU, beside the operands")
     return t
 
 
@@ -569,7 +569,7 @@ def group_norm_torch(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, a
     scale = torch.empty(N * S, -(-C // BLOCK), dtype=torch.float32, device=x.device) if codes else None
     op = GroupNorm(N, S, C, groups, eps=eps, act=act, x_type=x.dtype, y_type=y.dtype, x_strides=x.stride()[:2])
     ws, n = _workspace(op, x)
-    _call(op, x, x.data_ptr(), _ptr(_params(gamma, C, "gamma")), _ptr(_params(beta, C, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n)
+    _call(op, x, x.data_ptr(), _ptr(_params(gamma, C, x, "gamma")), _ptr(_params(beta, C, x, "beta")), y.data_ptr(), _ptr(scale), _ptr(ws), n)
     return (y, scale) if codes else y
 
 
@@ -600,7 +600,7 @@ def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dt
     y = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=a.device)
     op = BlockMatmul(M, N, K, y_type=y.dtype, act=act, a_row=a.stride(0), b_row=b.stride(0), a_scale_row=a_scale.stride(0), b_scale_row=b_scale.stride(0))
     ws, n = _workspace(op, a)
-    _call(op, a, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(_params(bias, N, "bias")), y.data_ptr(), _ptr(ws), n)
+    _call(op, a, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(_params(bias, N, a, "bias")), y.data_ptr(), _ptr(ws), n)
     return y
 
 
@@ -624,5 +624,5 @@ def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, 
                        a_scale_row=a_scale.stride(0) if codes else 0, b_scale_row=b_scale.stride(1) if codes else 0, b_scale_expert=b_scale.stride(0) if codes else 0)
     ws, n = _workspace(op, a)
     _call(op, a, a.data_ptr(), _ptr(a_scale if codes else None), _ptr(index), offsets.data_ptr(), b.data_ptr(), _ptr(b_scale if codes else None),
-          _ptr(_params(bias, E * N, "bias")), y.data_ptr(), _ptr(ws), n)
+          _ptr(_params(bias, E * N, a, "bias")), y.data_ptr(), _ptr(ws), n)
     return y

@@ -102,3 +102,15 @@ def test_convolutions_are_made_on_the_device_of_the_tensors(calls):
 
     y = B.forward_torch(Plan(), tensor(2, 3, 5, 5, dtype=torch.float32, device="cuda:1"))
     assert y.device == torch.device("cuda:1") and calls[0][2] == 1 and calls[0][1][-1] == 101
+
+
+def test_parameters_on_another_device_are_refused(calls):
+    there = tensor(64, dtype=torch.float32, device="cuda:1")
+    for pair in ((there, None), (None, there)):
+        with pytest.raises(ValueError):
+            B.group_norm_torch(tensor(2, 5, 64), 8, *pair)
+    with pytest.raises(ValueError):
+        B.matmul_blocks_torch(codes(3, 128), tensor(3, 1, dtype=torch.float32), codes(64, 128), tensor(1, 1, dtype=torch.float32), bias=there)
+    with pytest.raises(ValueError):
+        B.matmul_grouped_torch(tensor(3, 128), tensor(2, 32, 128), tensor(3, dtype=torch.int32), bias=there)
+    assert not calls
