@@ -506,7 +506,7 @@ def forward_torch(plan: Plan, x, y=None, workspace=None):
 
 
 # ... and of the operators of channels-last blocks: tensors in, tensors out, on their device and torch's current stream there.  Rows may lie further apart than
-# their length; the last dimension is contiguous.
+# their length; the last dimension is contiguous.  They have no gradient, and refuse tensors that want one.
 
 def _call(op, like, *args):
     """op.forward on the device where `like` lies, on torch's current stream there, whatever device is the current one."""
@@ -529,6 +529,12 @@ def _rows(t, what: str):
     if not t.is_cuda or t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{what}: a GPU tensor with a contiguous last dimension")
     return t
+
+
+def _forward_only(*tensors):
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("the operators have no gradient: call them under torch.no_grad(), or on detached tensors")
 
 
 def _params(t, n: int, like, what: str):
@@ -564,6 +570,7 @@ def group_norm_torch(x, groups: int, gamma=None, beta=None, eps: float = 1e-5, a
     """act(group norm) of x [N, S, C], channels last: a tensor like x, or with codes = True (e4m3 codes [N S, C], scales)."""
     import torch
     _rows(x, "x")
+    _forward_only(x, gamma, beta)
     N, S, C = x.shape
     y = empty_codes(N * S, C, device=x.device) if codes else torch.empty((N, S, C), dtype=x.dtype, device=x.device)
     scale = torch.empty(N * S, -(-C // BLOCK), dtype=torch.float32, device=x.device) if codes else None
@@ -577,6 +584,7 @@ def quantize_blocks_torch(x, rows: int = 1):
     """(e4m3 codes, scales) of a matrix [M, K] in blocks of rows x 128; a stack [E, M, K] matrix by matrix."""
     import torch
     _rows(x, "x")
+    _forward_only(x)
     lead, (M, K) = x.shape[:-2], x.shape[-2:]
     q = empty_codes(*lead, M, K, device=x.device)
     scale = torch.empty(*lead, -(-M // rows), -(-K // BLOCK), dtype=torch.float32, device=x.device)
@@ -591,6 +599,7 @@ def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dt
     import torch
     if _rows(a, "a").dim() != 2 or _rows(b, "b").dim() != 2:
         raise ValueError(f"a and b: matrices, not {list(a.shape)} and {list(b.shape)} (a stack of weights goes to matmul_grouped_torch)")
+    _forward_only(a, a_scale, b, b_scale, bias)
     (M, K), N = a.shape, b.shape[0]
     if b.shape[1] != K:
         raise ValueError(f"b has {b.shape[1]} columns, a has {K}")
@@ -609,6 +618,7 @@ def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, 
     codes with their scales; offsets and index 32-bit integers on the GPU."""
     import torch
     _rows(a, "a"), _rows(b, "b")
+    _forward_only(a, a_scale, b, b_scale, bias)
     E, N, K = b.shape
     if a.dim() != 2 or a.shape[1] != K or a.dtype != b.dtype or a.device != b.device or offsets.numel() != E + 1:
         raise ValueError("a [rows, K] and b [E, N, K] of one type on one GPU, offsets [E + 1]")

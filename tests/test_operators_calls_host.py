@@ -114,3 +114,33 @@ def test_parameters_on_another_device_are_refused(calls):
     with pytest.raises(ValueError):
         B.matmul_grouped_torch(tensor(3, 128), tensor(2, 32, 128), tensor(3, dtype=torch.int32), bias=there)
     assert not calls
+
+
+def test_tensors_that_want_a_gradient_are_refused(calls):
+    """The operators are forward only: a result without a gradient would end it silently.  Under no_grad nobody expects one."""
+    f32 = dict(dtype=torch.float32)
+    with_grad = lambda t: t.requires_grad_()  # noqa: E731
+    off = tensor(3, dtype=torch.int32)
+    a, b, sa, sb = codes(6, 256), codes(2, 64, 256), tensor(6, 2, **f32), tensor(2, 1, 2, **f32)
+    wanting = [
+        lambda: B.group_norm_torch(with_grad(tensor(2, 5, 64)), 8),
+        lambda: B.group_norm_torch(tensor(2, 5, 64), 8, gamma=with_grad(tensor(64, **f32))),
+        lambda: B.group_norm_torch(tensor(2, 5, 64), 8, beta=with_grad(tensor(64, **f32)), codes=True),
+        lambda: B.quantize_blocks_torch(with_grad(tensor(5, 64)), 128),
+        lambda: B.matmul_blocks_torch(a, with_grad(tensor(6, 2, **f32)), b[0], sb[0]),
+        lambda: B.matmul_blocks_torch(a, sa, b[0], with_grad(tensor(1, 2, **f32))),
+        lambda: B.matmul_blocks_torch(a, sa, b[0], sb[0], bias=with_grad(tensor(64, **f32))),
+        lambda: B.matmul_grouped_torch(with_grad(tensor(6, 128)), tensor(2, 64, 128), off),
+        lambda: B.matmul_grouped_torch(tensor(6, 128), with_grad(tensor(2, 64, 128)), off),
+        lambda: B.matmul_grouped_torch(a, b, off, with_grad(tensor(6, 2, **f32)), sb),
+        lambda: B.matmul_grouped_torch(a, b, off, sa, with_grad(tensor(2, 1, 2, **f32))),
+        lambda: B.matmul_grouped_torch(a, b, off, sa, sb, bias=with_grad(tensor(2, 64, **f32))),
+    ]
+    for i, call in enumerate(wanting):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        assert not calls, i
+    with torch.no_grad():
+        for call in wanting:
+            call()
+    assert len(calls) == len(wanting)
