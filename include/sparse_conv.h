@@ -584,6 +584,34 @@ typedef struct {
 
 sc_status_t sparse_conv_matmul_grouped_workspace_size(const sc_matmul_grouped_t* d, size_t* bytes);
 
+/* What a call with this description runs, as the call itself decides it: host only, nothing is launched.  For tests that
+ * have to reach every form, and for reports of timings.  The numbers are no promise: a form may change with the library. */
+typedef enum {
+    SC_FORM_NOTHING = 0,             /* no rows */
+    SC_FORM_NORM_LANES = 1,          /* one launch, groups of a power of two of lanes */
+    SC_FORM_NORM_SAMPLE = 2,         /* one launch, groups of any size, samples or parts of them */
+    SC_FORM_NORM_TWO = 3,            /* statistics, then the result */
+    SC_FORM_ROWS = 4,                /* 16 x 16 of y a workgroup */
+    SC_FORM_TILE_64 = 5,
+    SC_FORM_TILE_64_SPLIT = 6,       /* two groups of waves share the summed dimension */
+    SC_FORM_TILE_128 = 7,
+    SC_FORM_TILE_128_DEEP = 8,       /* four slabs in LDS */
+    SC_FORM_TILE_256 = 9
+} sc_form_t;
+
+typedef struct {
+    int32_t form;                    /* sc_form_t */
+    int32_t lanes;                   /* group norm in one launch: lanes of a workgroup, */
+    int32_t held;                    /* ... 16-byte vectors that a lane holds, */
+    int32_t one_die;                 /* ... the parts of a sample on one die, */
+    int32_t past_cache;              /* ... x read past the last-level cache */
+} sc_launch_t;
+
+/* Errors: those of the description. */
+sc_status_t sparse_conv_group_norm_launch(const sc_group_norm_t* d, sc_launch_t* launch);
+sc_status_t sparse_conv_matmul_blocks_launch(const sc_matmul_blocks_t* d, sc_launch_t* launch);
+sc_status_t sparse_conv_matmul_grouped_launch(const sc_matmul_grouped_t* d, sc_launch_t* launch);
+
 /*   a, b device, as for sparse_conv_matmul_blocks     a_scale, b_scale E4M3 only
  *   index device i32 [M] or NULL     offsets device i32 [E + 1]     bias device f32 [E][N] or NULL
  * Errors: as sparse_conv_matmul_blocks; SC_ERR_RANGE also for experts 2^48 elements or more apart. */

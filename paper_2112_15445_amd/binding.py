@@ -29,6 +29,7 @@ SC_ELEM_F32, SC_ELEM_F16, SC_ELEM_BF16, SC_ELEM_E4M3 = 0, 1, 2, 3
 ELEMS = {"f32": SC_ELEM_F32, "f16": SC_ELEM_F16, "bf16": SC_ELEM_BF16, "e4m3": SC_ELEM_E4M3}
 SC_ACT_NONE, SC_ACT_RELU, SC_ACT_SILU = 0, 1, 2
 ACTS = {"none": SC_ACT_NONE, "relu": SC_ACT_RELU, "silu": SC_ACT_SILU}
+FORMS = ["nothing", "norm lanes", "norm sample", "norm two", "rows", "64", "64 split", "128", "128 deep", "256"]   # SC_FORM_*
 BLOCK = 128                        # elements of a row that share a scale
 
 # every symbol include/sparse_conv.h declares
@@ -42,6 +43,7 @@ EXPORTS = [
     "sparse_conv_group_norm_workspace_size", "sparse_conv_group_norm", "sparse_conv_quantize_blocks",
     "sparse_conv_matmul_blocks_workspace_size", "sparse_conv_matmul_blocks",
     "sparse_conv_matmul_grouped_workspace_size", "sparse_conv_matmul_grouped",
+    "sparse_conv_group_norm_launch", "sparse_conv_matmul_blocks_launch", "sparse_conv_matmul_grouped_launch",
 ]
 
 
@@ -111,6 +113,10 @@ class sc_matmul_grouped_t(ctypes.Structure):
                        ("a_row", "b_row", "b_expert", "y_row", "a_scale_row", "b_scale_row", "b_scale_expert"))
 
 
+class sc_launch_t(ctypes.Structure):
+    _fields_ = _fields(("form", "lanes", "held", "one_die", "past_cache"), (), (), ())
+
+
 class SparseConvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -163,6 +169,9 @@ def lib() -> ctypes.CDLL:
     L.sparse_conv_matmul_blocks_workspace_size.argtypes = [P(sc_matmul_blocks_t), P(sz)]
     L.sparse_conv_matmul_blocks.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.sparse_conv_matmul_grouped_workspace_size.argtypes = [P(sc_matmul_grouped_t), P(sz)]
+    L.sparse_conv_group_norm_launch.argtypes = [P(sc_group_norm_t), P(sc_launch_t)]
+    L.sparse_conv_matmul_blocks_launch.argtypes = [P(sc_matmul_blocks_t), P(sc_launch_t)]
+    L.sparse_conv_matmul_grouped_launch.argtypes = [P(sc_matmul_grouped_t), P(sc_launch_t)]
     L.sparse_conv_matmul_grouped.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("sparse_conv_plan_destroy", "sparse_conv_status_string"):
@@ -385,6 +394,13 @@ class _Operator:
         name = self._name + "_workspace_size"
         _check(getattr(lib(), name)(ctypes.byref(self.desc), ctypes.byref(b)), name)
         return int(b.value)
+
+    def launch(self) -> dict:
+        """What a call runs: "form" (one of FORMS) and, of a group norm in one launch, "lanes", "held", "one_die", "past_cache"."""
+        l = sc_launch_t()
+        name = self._name + "_launch"
+        _check(getattr(lib(), name)(ctypes.byref(self.desc), ctypes.byref(l)), name)
+        return {k: FORMS[l.form] if k == "form" else int(getattr(l, k)) for k, _ in l._fields_}
 
     def _refused(self, status):
         raise SparseConvError(status, self._name)

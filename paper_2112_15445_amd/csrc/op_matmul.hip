@@ -32,44 +32,45 @@ template <int AT, int YT, bool GROUPED> sc_status_t launch_rows(const MatmulArgs
 // groups, 200 to 3200 columns and 256 to 4096 summed values in every pair of types; there the choice costs 2.1 % more than the fastest form
 // each time, without the split 64 tile 3.2 %; on 199 of them, timed again, 1.7 %, without the widest 2.3 %, the deep one 2.7 %, the 64 or the 128
 // tile 6 %.  Groups: half a tile more each, and one each at least where they have rows (2.0 % on 140 of them, 2.5 % without the latter).
-enum Form { kRows, kTile64, kTile64Split, kTile128, kTile128Deep, kTile256 };
-struct TileTime { Form form; int size, places; double start, slab, slab_half_empty; };
-constexpr TileTime kTiles[] = {{kTile64, 64, 512, 1.5, 0.41, 0.20},
-                               {kTile64Split, 64, 256, 2.3, 0.24, 0.16},
-                               {kTile128, 128, 512, 3.6, 0.88, 0.67},
-                               {kTile128Deep, 128, 256, 2.2, 0.62, 0.50},
-                               {kTile256, 256, 256, 6.2, 1.38, 1.25}};
+struct TileTime { sc_form_t form; int size, places; double start, slab, slab_half_empty; };
+constexpr TileTime kTiles[] = {{SC_FORM_TILE_64, 64, 512, 1.5, 0.41, 0.20},
+                               {SC_FORM_TILE_64_SPLIT, 64, 256, 2.3, 0.24, 0.16},
+                               {SC_FORM_TILE_128, 128, 512, 3.6, 0.88, 0.67},
+                               {SC_FORM_TILE_128_DEEP, 128, 256, 2.2, 0.62, 0.50},
+                               {SC_FORM_TILE_256, 256, 256, 6.2, 1.38, 1.25}};
 
-Form pick_form(const MatmulArgs& p, bool grouped, bool widest)
+sc_form_t pick_form(const MatmulArgs& p, bool grouped, bool widest)
 {
     const int64_t columns16 = ceil_div(p.N, 16), slabs = ceil_div(p.kbytes, kSlab);
-    if (grouped ? (ceil_div(p.M, 16) + std::min(p.E, p.M)) * columns16 <= 512 : p.M <= 16 || ceil_div(p.M, 16) * columns16 <= 512) return kRows;
-    Form best = kRows;
+    if (grouped ? (ceil_div(p.M, 16) + std::min(p.E, p.M)) * columns16 <= 512 : p.M <= 16 || ceil_div(p.M, 16) * columns16 <= 512) return SC_FORM_ROWS;
+    sc_form_t best = SC_FORM_ROWS;
     double least = 0.0;
     for (const TileTime& t : kTiles) {
-        if (t.form == kTile256 && !widest) continue;
+        if (t.form == SC_FORM_TILE_256 && !widest) continue;
         const double even = (double)ceil_div(p.M, t.size), rows = grouped ? std::max(even + 0.5 * p.E, (double)std::min(p.E, p.M)) : even;
         const double tiles = std::ceil(rows) * (double)ceil_div(p.N, t.size);
         const double full = std::floor(tiles / t.places), rest = tiles - full * t.places;
         const double last = rest == 0.0 ? 0.0 : rest <= 0.5 * t.places ? t.slab_half_empty : t.slab;
         const double time = std::max(7.2, 3.0 + slabs * (full * t.slab + last) + (full + (rest > 0.0)) * t.start);
-        if (best == kRows || time < least) best = t.form, least = time;
+        if (best == SC_FORM_ROWS || time < least) best = t.form, least = time;
     }
     return best;
 }
 
+// (32-bit results of codes keep both operands widened in registers: the widest tile has none left)
+constexpr bool has_widest(int a_type, int y_type) { return a_type != SC_ELEM_E4M3 || y_type != SC_ELEM_F32; }
+
 template <int AT, int YT, bool GROUPED> sc_status_t launch(const MatmulArgs& p, hipStream_t stream)
 {
-    // (32-bit results of codes keep both operands widened in registers: the widest tile has none left)
-    constexpr bool WIDEST = AT != SC_ELEM_E4M3 || YT != SC_ELEM_F32;
+    constexpr bool WIDEST = has_widest(AT, YT);
     switch (pick_form(p, GROUPED, WIDEST)) {
-        case kRows: return launch_rows<AT, YT, GROUPED>(p, stream);
-        case kTile64: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 4>(p, stream);
-        case kTile64Split: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 3, 2>(p, stream);
+        case SC_FORM_ROWS: return launch_rows<AT, YT, GROUPED>(p, stream);
+        case SC_FORM_TILE_64: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 4>(p, stream);
+        case SC_FORM_TILE_64_SPLIT: return launch_tile<AT, YT, GROUPED, 64, 64, 2, 2, 3, 2>(p, stream);
         // (eight waves where their registers leave room for a second workgroup: 3 % less than four over 68 products; 7 % more in 32-bit
         // results of codes)
-        case kTile128: return launch_tile<AT, YT, GROUPED, 128, 128, WIDEST ? 4 : 2, 2, 2>(p, stream);
-        case kTile128Deep: return launch_tile<AT, YT, GROUPED, 128, 128, 4, 2, 4>(p, stream);
+        case SC_FORM_TILE_128: return launch_tile<AT, YT, GROUPED, 128, 128, WIDEST ? 4 : 2, 2, 2>(p, stream);
+        case SC_FORM_TILE_128_DEEP: return launch_tile<AT, YT, GROUPED, 128, 128, 4, 2, 4>(p, stream);
         default: break;
     }
     if constexpr (WIDEST) return launch_tile<AT, YT, GROUPED, 256, 256, 4, 2, 2>(p, stream);
@@ -107,6 +108,21 @@ sc_status_t check_grouped(const sc_matmul_grouped_t* d)
     return SC_OK;
 }
 
+// What the choice of a form goes by.
+MatmulArgs sizes(const sc_matmul_blocks_t* d)
+{
+    MatmulArgs p{};
+    p.M = d->M; p.N = d->N; p.E = 1; p.kbytes = d->K;
+    return p;
+}
+
+MatmulArgs sizes(const sc_matmul_grouped_t* d)
+{
+    MatmulArgs p{};
+    p.M = d->M; p.N = d->N; p.E = d->E; p.kbytes = d->K * elem_bytes(d->a_type);
+    return p;
+}
+
 }  // namespace
 }  // namespace sc
 
@@ -120,6 +136,16 @@ extern "C" sc_status_t sparse_conv_matmul_blocks_workspace_size(const sc_matmul_
     return st;
 }
 
+extern "C" sc_status_t sparse_conv_matmul_blocks_launch(const sc_matmul_blocks_t* d, sc_launch_t* launch)
+{
+    if (!launch) return SC_ERR_NULL;
+    const sc_status_t st = check_blocks(d);
+    if (st != SC_OK) return st;
+    *launch = sc_launch_t{};
+    if (d->M) launch->form = pick_form(sizes(d), false, has_widest(SC_ELEM_E4M3, d->y_type));
+    return SC_OK;
+}
+
 extern "C" sc_status_t sparse_conv_matmul_blocks(const sc_matmul_blocks_t* d, const void* a, const float* a_scale, const void* b,
                                                  const float* b_scale, const float* bias, void* y, void* workspace_dev,
                                                  size_t workspace_bytes, void* stream)
@@ -131,9 +157,9 @@ extern "C" sc_status_t sparse_conv_matmul_blocks(const sc_matmul_blocks_t* d, co
     if (!a || !a_scale || !b || !b_scale || !y) return SC_ERR_NULL;
     if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(bias, 4) || !aligned(y, elem_bytes(d->y_type)))
         return SC_ERR_UNSUPPORTED;
-    MatmulArgs p{};
+    MatmulArgs p = sizes(d);
     p.a = static_cast<const uint8_t*>(a); p.b = static_cast<const uint8_t*>(b); p.as = a_scale; p.bs = b_scale; p.bias = bias; p.y = y;
-    p.M = d->M; p.N = d->N; p.E = 1; p.a_rows = d->M; p.kbytes = d->K;
+    p.a_rows = d->M;
     p.a_row = d->a_row; p.b_row = d->b_row; p.y_row = d->y_row; p.as_row = d->a_scale_row; p.bs_row = d->b_scale_row; p.act = d->act;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (d->y_type) {
@@ -151,6 +177,16 @@ extern "C" sc_status_t sparse_conv_matmul_grouped_workspace_size(const sc_matmul
     return st;
 }
 
+extern "C" sc_status_t sparse_conv_matmul_grouped_launch(const sc_matmul_grouped_t* d, sc_launch_t* launch)
+{
+    if (!launch) return SC_ERR_NULL;
+    const sc_status_t st = check_grouped(d);
+    if (st != SC_OK) return st;
+    *launch = sc_launch_t{};
+    if (d->M) launch->form = pick_form(sizes(d), true, has_widest(d->a_type, d->y_type));
+    return SC_OK;
+}
+
 extern "C" sc_status_t sparse_conv_matmul_grouped(const sc_matmul_grouped_t* d, const void* a, const float* a_scale,
                                                   const int32_t* index, const int32_t* offsets, const void* b, const float* b_scale,
                                                   const float* bias, void* y, void* workspace_dev, size_t workspace_bytes, void* stream)
@@ -166,10 +202,10 @@ extern "C" sc_status_t sparse_conv_matmul_grouped(const sc_matmul_grouped_t* d, 
         !aligned(y, elem_bytes(d->y_type)))
         return SC_ERR_UNSUPPORTED;
     const int e = elem_bytes(d->a_type);
-    MatmulArgs p{};
+    MatmulArgs p = sizes(d);
     p.a = static_cast<const uint8_t*>(a); p.b = static_cast<const uint8_t*>(b); p.as = a_scale; p.bs = b_scale; p.bias = bias;
     p.index = index; p.offsets = offsets; p.y = y;
-    p.M = d->M; p.N = d->N; p.E = d->E; p.a_rows = d->a_rows; p.kbytes = d->K * e;
+    p.a_rows = d->a_rows;
     p.a_row = d->a_row * e; p.b_row = d->b_row * e; p.b_expert = d->E > 1 ? d->b_expert * e : 0; p.y_row = d->y_row;
     p.as_row = d->a_scale_row; p.bs_row = d->b_scale_row; p.bs_expert = d->b_scale_expert; p.act = d->act;
     const hipStream_t s = static_cast<hipStream_t>(stream);

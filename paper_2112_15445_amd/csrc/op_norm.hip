@@ -35,7 +35,7 @@ struct NormArgs {
     int seg, segs, parts;                    // channels of a workgroup of whole samples' parts, or of the statistics, segments of C, segments of one group (1: whole groups)
     int len, stretches;                      // positions of a stretch, stretches of a sample
     int rows;                                // positions of a workgroup of the second launch
-    int once;                                // x and y do not stay in the last-level cache side by side: x passes it by
+    int once;                                // x passes the last-level cache by
     float eps;
     int64_t x_sample, x_row, y_sample, y_row, s_row;
 };
@@ -618,6 +618,10 @@ NormShape norm_shape(const sc_group_norm_t* d)
     return s;
 }
 
+// Whether x and y do not stay in the last-level cache side by side: x passes it by then.
+// (32 x 56x56 x 256 fp32, 206 MB: 47 us with the hint and 52 without; 39 MB of a quantiser's: 11.0 with and 10.4 without)
+bool past_cache(const sc_group_norm_t* d) { return (int64_t)d->N * d->S * d->C * (elem_bytes(d->x_type) + elem_bytes(d->y_type)) > (int64_t)128 << 20; }
+
 sc_status_t check_norm(const sc_group_norm_t* d)
 {
     if (!d) return SC_ERR_NULL;
@@ -691,6 +695,22 @@ extern "C" sc_status_t sparse_conv_group_norm_workspace_size(const sc_group_norm
     return SC_OK;
 }
 
+extern "C" sc_status_t sparse_conv_group_norm_launch(const sc_group_norm_t* d, sc_launch_t* launch)
+{
+    if (!launch) return SC_ERR_NULL;
+    const sc_status_t st = check_norm(d);
+    if (st != SC_OK) return st;
+    *launch = sc_launch_t{};
+    if (d->N == 0 || d->S == 0) return SC_OK;
+    const NormShape s = norm_shape(d);
+    launch->form = !s.T ? SC_FORM_NORM_TWO : s.TPR ? SC_FORM_NORM_LANES : SC_FORM_NORM_SAMPLE;
+    launch->lanes = s.T;
+    launch->held = s.U;
+    launch->one_die = s.T ? s.dies : 0;
+    launch->past_cache = s.T && s.TPR && past_cache(d);
+    return SC_OK;
+}
+
 extern "C" sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const void* x, const float* gamma, const float* beta,
                                               void* y, float* y_scale, void* workspace_dev, size_t workspace_bytes, void* stream)
 {
@@ -709,8 +729,7 @@ extern "C" sc_status_t sparse_conv_group_norm(const sc_group_norm_t* d, const vo
     a.N = d->N; a.S = d->S; a.C = d->C; a.G = d->G; a.Cg = d->C / d->G;
     a.seg = shape.seg; a.segs = shape.segs; a.parts = shape.parts; a.len = shape.len; a.stretches = shape.stretches; a.rows = shape.rows;
     a.eps = d->eps;
-    // (32 x 56x56 x 256 fp32, 206 MB: 47 us with the hint and 52 without; 39 MB of a quantiser's: 11.0 with and 10.4 without)
-    a.once = (int64_t)d->N * d->S * d->C * (elem_bytes(d->x_type) + elem_bytes(d->y_type)) > (int64_t)128 << 20;
+    a.once = past_cache(d);
     a.x_sample = d->x_sample; a.x_row = d->x_row; a.y_sample = d->y_sample; a.y_row = d->y_row; a.s_row = d->scale_row;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (d->x_type) {
