@@ -50,3 +50,12 @@ def test_the_quantiser_refuses_columns_that_its_counters_pass(K, rows):
     """Columns are counted in 32 bits, up to the end of the last block and to the next multiple of 16."""
     refused(RANGE, B.BlockQuantizer(1, K, rows=rows), P, P, P)
     B.BlockQuantizer(0, (1 << 31) - 256, rows=rows).forward(0, 0, 0)
+
+
+@pytest.mark.parametrize("shape,x_type,y_type", [((2, 3000, 48, 3), "f16", None), ((1, 500, 360, 30), "f16", "e4m3"), ((32, 3136, 256, 32), "bf16", "e4m3"), ((1, 5000, 7, 1), "f32", None)])
+def test_group_norm_in_two_launches_refuses_workspaces_that_do_not_do(shape, x_type, y_type):
+    op = B.GroupNorm(*shape, x_type=x_type, y_type=y_type)
+    need = op.workspace_size()
+    assert need > 0 and op.launch()["form"] == "norm two"
+    for ws, size in ((0, 0), (0, need), (P, 0), (P, need - 1), (P + 4, need), (P + 8, need + 8)):
+        refused(WORKSPACE, op, P, P, P, P, P, ws, size)
