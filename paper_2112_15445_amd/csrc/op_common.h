@@ -30,10 +30,30 @@ inline bool is_wide(int et) { return et == SC_ELEM_F32 || et == SC_ELEM_F16 || e
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <int ACT> __device__ __forceinline__ float activate(float z)
+// z / (1 + exp(-z)) within some 2 ulp of 32 bits, from e = exp(-|z|) <= 1, which overflows nothing: z / (1 + e), or z e / (1 + e) where z is
+// negative.  e = 2^t for t = -|z| log2(e), with what rounding t left out (its own, and the constant's lower half) put back by 2^r = 1 + r ln 2; the
+// reciprocal of 1 .. 2 with one step of Newton's.  |z| is cut off where e is 0 (an infinite one would make r a NaN); below -87.3, e and the result are 0.
+// Group norm of 32 x 56x56 x 256 fp32 52 us, product 8192 x 4096 x 1024 -> fp32 85 (with expf and a division 57 and 94, as for 16 bits 48 and 81).
+__device__ __forceinline__ float silu32(float z)
+{
+    constexpr float kLog2e = 0x1.715476p+0f, kLog2eLow = 0x1.4ae0c0p-26f, kLn2 = 0x1.62e430p-1f;
+    const float m = -fminf(fabsf(z), 200.0f), t = m * kLog2e;
+    const float r = fmaf(m, kLog2eLow, fmaf(m, kLog2e, -t));
+    float e = __builtin_amdgcn_exp2f(t);
+    e = fmaf(e, r * kLn2, e);
+    const float d = 1.0f + e;
+    float inv = __builtin_amdgcn_rcpf(d);
+    inv = fmaf(fmaf(-d, inv, 1.0f), inv, inv);
+    return (z < 0.0f ? z * e : z) * inv;
+}
+
+// YT: type of the result.  What is rounded to 16 bits or to codes after SiLU takes the exponential through the product z log2(e), off by |z| 2^-23
+// of the result (5e-6 at z = -40, where f16 rounds by 5e-4 of it), and a reciprocal right to one place (a scale of codes, 32 bits, is off by no more).
+template <int ACT, int YT> __device__ __forceinline__ float activate(float z)
 {
     if constexpr (ACT == SC_ACT_RELU) return z < 0.0f ? 0.0f : z;      // (NaN stays NaN)
-    else if constexpr (ACT == SC_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));   // (the reciprocal is right to one place; a division takes ten instructions)
+    else if constexpr (ACT == SC_ACT_SILU && YT == SC_ELEM_F32) return silu32(z);
+    else if constexpr (ACT == SC_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
     else return z;
 }
 

@@ -70,20 +70,20 @@ __device__ __forceinline__ v8h widen8(int lo, int hi)
     return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-__device__ __forceinline__ float act_of(float z, int act)
+template <int YT> __device__ __forceinline__ float act_of(float z, int act)
 {
-    return act == SC_ACT_RELU ? activate<SC_ACT_RELU>(z) : act == SC_ACT_SILU ? activate<SC_ACT_SILU>(z) : z;
+    return act == SC_ACT_RELU ? activate<SC_ACT_RELU, YT>(z) : act == SC_ACT_SILU ? activate<SC_ACT_SILU, YT>(z) : z;
 }
 
 // Eight of them after one branch (a branch each: a tile of 256 x 256 leaves by 41 KB of code for 27, experts' products take 1.5 % more).
-__device__ __forceinline__ void act_all(float (&z)[8], int act)
+template <int YT> __device__ __forceinline__ void act_all(float (&z)[8], int act)
 {
     if (act == SC_ACT_RELU) {
 #pragma unroll
-        for (int v = 0; v < 8; ++v) z[v] = activate<SC_ACT_RELU>(z[v]);
+        for (int v = 0; v < 8; ++v) z[v] = activate<SC_ACT_RELU, YT>(z[v]);
     } else if (act == SC_ACT_SILU) {
 #pragma unroll
-        for (int v = 0; v < 8; ++v) z[v] = activate<SC_ACT_SILU>(z[v]);
+        for (int v = 0; v < 8; ++v) z[v] = activate<SC_ACT_SILU, YT>(z[v]);
     }
 }
 
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(Matmu
             float z[8];
 #pragma unroll
             for (int v = 0; v < 8; ++v) z[v] = (zero[j] ? 0.0f : acc[i + (v >> 2)][j][v & 3]) + add[v];
-            act_all(z, p.act);
+            act_all<YT>(z, p.act);
             if (wide && whole8) {
                 store_vec_past<YT, 8>(y, z);
             } else {
@@ -577,7 +577,7 @@ template <int AT, int YT, bool GROUPED> __global__ __launch_bounds__(512) void m
         if constexpr (GROUPED)
             if (p.index && (uint32_t)p.index[m0 + r] >= (uint32_t)p.a_rows) s = 0.0f;
         if (bias) s += bias[n];
-        static_cast<Elem<YT>*>(p.y)[(m0 + r) * p.y_row + n] = (Elem<YT>)act_of(s, p.act);
+        static_cast<Elem<YT>*>(p.y)[(m0 + r) * p.y_row + n] = (Elem<YT>)act_of<YT>(s, p.act);
     }
 }
 

@@ -58,11 +58,11 @@ template <int V> __device__ __forceinline__ void load_params(float* out, const f
 __device__ __forceinline__ int small_div(int i, float inv) { return (int)(((float)i + 0.5f) * inv); }
 
 // y of V neighbouring channels of one position; gam: gamma over the spread.
-template <int ACT, int V>
+template <int ACT, int YT, int V>
 __device__ __forceinline__ void finish(float* f, const float* mean, const float* gam, const float* bet, int have)
 {
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = i < have ? activate<ACT>((f[i] - mean[i]) * gam[i] + bet[i]) : 0.0f;
+    for (int i = 0; i < V; ++i) f[i] = i < have ? activate<ACT, YT>((f[i] - mean[i]) * gam[i] + bet[i]) : 0.0f;
 }
 
 // The sample and part of this workgroup, of `parts` a sample.  dies: those of a sample go to one die, one after another, so that the pieces
@@ -156,7 +156,7 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
         if (pos >= a.S) continue;            // (a position's lanes go on or leave together: the shuffles below stay inside it)
         float f[V];
         to_floats<XT>(raw[u], f);
-        finish<ACT, V>(f, means, gam, bet, V);
+        finish<ACT, YT, V>(f, means, gam, bet, V);
         Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c;
         if constexpr (YT == SC_ELEM_E4M3) {
             constexpr int L = kQBlock / V;
@@ -290,7 +290,7 @@ template <int XT, int YT, int ACT, int T, int U> __global__ __launch_bounds__(T,
         if (pos >= rows) continue;                   // (the lanes of a position go on or leave together)
         float f[V];
         to_floats<XT>(raw[u], f);
-        finish<ACT, V>(f, mean, gam, bet, have);
+        finish<ACT, YT, V>(f, mean, gam, bet, have);
         Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + n * a.y_sample + pos * a.y_row + c0 + c;
         if constexpr (CODES) {
             float amax = kAmaxFloor;
@@ -476,7 +476,7 @@ template <int XT, int YT, int ACT> __global__ __launch_bounds__(kThreads) void n
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             to_floats<XT>(now[u], f[u]);
-            finish<ACT, V>(f[u], mean, gam, bet, have);
+            finish<ACT, YT, V>(f[u], mean, gam, bet, have);
             if constexpr (CODES) {
                 amax[u] = kAmaxFloor;
 #pragma unroll

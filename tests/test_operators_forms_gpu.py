@@ -171,6 +171,58 @@ def test_products_keep_what_is_not_finite_in_its_row_and_column(form, y_type):
     assert np.all(np.isnan(got[r[:2]])) and np.all(np.isnan(got[:, c])) and not np.any(np.isfinite(got[r[2]]))
 
 
+# -- SiLU ------------------------------------------------------------------------------------------
+
+def silu_is_right(z, y, y_type, what):
+    """z / (1 + exp(-z)) of 32-bit z, relative to itself, for z of -87 and more.
+
+    f32: the exponential within 2 ulp (2^-22), one addition, one division: 1.5 * 2^-22.  16 bits: their own rounding; the exponential
+    through a 32-bit product z log2(e), whose rounding and constant count |z| 2^-24 each, and a reciprocal, both within one ulp: 2^-21 with
+    the rest; numbers below the type's normal ones are not compared."""
+    z = z.astype(np.float64)
+    ref = z / (1 + np.exp(-z))
+    if y_type == "f32":
+        allowed = 1.5 * 2.0 ** -22 * np.ones_like(z)
+    else:
+        allowed = O.ROUND[y_type][0] * (1 + 2.0 ** -8) + 2.0 ** -21 + 2 * np.abs(z) * 2.0 ** -24
+    normal = np.abs(ref) >= (2.0 ** -14 if y_type == "f16" else 2.0 ** -126)
+    off = np.abs(y - ref)[normal] / np.abs(ref)[normal] / allowed[normal]
+    assert off.max() <= 1, (what, y_type, z[normal][off.argmax()], off.max())
+
+
+@pytest.mark.parametrize("y_type", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("S,C,G,form", [(49, 256, 32, "norm lanes"), (4, 844, 1, "norm sample"), (3000, 48, 3, "norm two")])
+def test_silu_of_the_norm_relative_to_itself(S, C, G, form, y_type):
+    """gamma = 0 makes z beta exactly."""
+    z = torch.linspace(-87, 87, C).cuda()
+    x = torch.randn(2, S, C, device="cuda").to(T.T[y_type])
+    op = B.GroupNorm(2, S, C, G, x_type=y_type, act="silu")
+    assert op.launch()["form"] == form
+    y = B.group_norm_torch(x, G, torch.zeros(C, device="cuda"), z, act="silu")
+    assert torch.equal(y, y[:1, :1].expand_as(y))
+    silu_is_right(T.host(z), T.host(y[0, 0]), y_type, form)
+
+
+@pytest.mark.parametrize("y_type", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("form", list(PRODUCTS))
+def test_silu_of_products_relative_to_itself(form, y_type):
+    """Rows of zero codes make z the bias exactly."""
+    if form == "256" and y_type == "f32":
+        return
+    M, N, K = PRODUCTS[form]
+    (qa, sa), (qb, sb) = B.quantize_blocks_torch(torch.zeros(M, K, device="cuda")), B.quantize_blocks_torch(torch.randn(N, K, device="cuda"), 128)
+    z = torch.linspace(-87, 87, N).cuda()
+    y = B.matmul_blocks_torch(qa, sa, qb, sb, bias=z, act="silu", dtype=T.T[y_type])
+    assert torch.equal(y, y[:1].expand_as(y))
+    silu_is_right(T.host(z), T.host(y[0]), y_type, form)
+    off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    a = torch.zeros(M, K, device="cuda", dtype=torch.float16)
+    b = torch.randn(1, N, K, device="cuda").half()
+    if K % 8 == 0 and y_type in ("f32", "f16"):
+        y = B.matmul_grouped_torch(a, b, off, bias=z, act="silu", dtype=T.T[y_type])
+        silu_is_right(T.host(z), T.host(y[M - 1]), y_type, form + " by expert")
+
+
 # -- streams and graphs ------------------------------------------------------------------------------
 
 def calls():
