@@ -631,7 +631,7 @@ def matmul_blocks_torch(a, a_scale, b, b_scale, bias=None, act: str = "none", dt
 
 def matmul_grouped_torch(a, b, offsets, a_scale=None, b_scale=None, index=None, bias=None, act: str = "none", dtype=None):
     """Rows offsets[e] .. offsets[e+1] - 1 of the result: act(a[index] b[e]^T + bias[e]); a [rows, K], b [E, N, K], f16, bf16 or
-    codes with their scales; offsets and index 32-bit integers on the GPU."""
+    codes with their scales; offsets and index 32-bit integers on the GPU.  Rows outside all groups are left as they were allocated."""
     import torch
     _rows(a, "a"), _rows(b, "b")
     _forward_only(a, a_scale, b, b_scale, bias)

@@ -496,6 +496,8 @@ __global__ __launch_bounds__(WT * WN * KS * 64, 2) void matmul_tile_kernel(Matmu
 #pragma unroll
             for (int v = 0; v < 8; ++v) z[v] = (zero[j] ? 0.0f : acc[i + (v >> 2)][j][v & 3]) + add[v];
             act_all<YT>(z, p.act);
+            // (Past the caches: 6272 x 1024 x 256 -> f16 7.2 us for 8.1, with a quantiser of the result behind it 14.5 for 16.2; 16384 x 4096 x 2048,
+            // 134 MB of results, 139 for 132, with the quantiser 172 for 163.)
             if (wide && whole8) {
                 store_vec_past<YT, 8>(y, z);
             } else {
