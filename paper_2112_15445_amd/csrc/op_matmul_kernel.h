@@ -172,7 +172,9 @@ __device__ __forceinline__ int lane_key(int c) { return ((c >> 1) & 1) | ((c >> 
 __device__ __forceinline__ int token_key(int row) { return lane_key(row & 15); }
 __device__ __forceinline__ int weight_key(int row) { return lane_key((row & 3) | ((row >> 1) & 12)); }
 
-// One block's product of codes, unscaled: 16 weight rows (x) and 16 rows of a (z).
+// One block's product of codes, unscaled: 16 weight rows (x) and 16 rows of a (z).  For 32-bit results exact products and 32-bit sums.  For 16-bit ones
+// the 8-bit instruction, twice as fast: inside it what lies 13 bits below the largest of some eight products is cut off, which leaves 1.4e-5 of the
+// result, 3.4e-5 with one value of the block a hundred times the others, where f16 rounds by 2e-4; blocks are added in 32 bits either way.
 template <int YT> __device__ __forceinline__ v4f block_product(const v4i* x, const v4i* z)
 {
     v4f d = {0, 0, 0, 0};
