@@ -334,7 +334,9 @@ template <int XT, int YT, int KT> __global__ __launch_bounds__(kUpWaves * 64, KT
     int at[KT];
 #pragma unroll
     for (int k = 0; k < KT; ++k) at[k] = min(k * 64 + q * 16, (p.R * 2 - 1) & ~15);
-    const v4i keep = first_bytes(v4i{-1, -1, -1, -1}, p.R * 2 - (KT - 1) * 64 - q * 16);
+    // (the step in which a row ends is one of the later half: what is kept of it; of the steps behind it, nothing)
+    const int tail = (p.R * 2 - 1) >> 6;
+    const v4i keep = first_bytes(v4i{-1, -1, -1, -1}, p.R * 2 - tail * 64 - q * 16);
     const Elem<YT>* from = static_cast<const Elem<YT>*>(p.base) + token * p.base_row + q * 8;
     Elem<YT>* to = static_cast<Elem<YT>*>(p.y) + token * p.y_row + q * 8;
     struct Pair { v4i w[2][KT]; float base[8]; };
@@ -381,7 +383,10 @@ template <int XT, int YT, int KT> __global__ __launch_bounds__(kUpWaves * 64, KT
     auto finish = [&](int n, Pair& o) {
         v4f acc[2] = {};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) o.w[i][KT - 1] &= keep;
+        for (int k = KT / 2; k < KT; ++k)
+            if (k >= tail)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) o.w[i][k] = k == tail ? o.w[i][k] & keep : v4i{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
@@ -433,13 +438,13 @@ template <int XT, int YT, int KT> __global__ __launch_bounds__(kWideWaves * 64) 
     // b of the wave's columns: of two products a lane's sums are those of eight neighbouring columns (see the tile of the products).  What lies behind a row's end
     // is read from its last sixteen bytes, and dropped.
     v4i w[NP][KT];
-    const v4i keep = first_bytes(v4i{-1, -1, -1, -1}, p.R * 2 - (KT - 1) * 64 - q * 16);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const uint8_t* row = p.b + e * p.b_adapter + min(n0 + (i >> 1) * 32 + (c >> 2) * 8 + (i & 1) * 4 + (c & 3), p.N - 1) * p.b_row;
 #pragma unroll
         for (int k = 0; k < KT; ++k) w[i][k] = *reinterpret_cast<const v4i*>(row + min(k * 64 + q * 16, (p.R * 2 - 1) & ~15));
-        w[i][KT - 1] &= keep;
+#pragma unroll
+        for (int k = KT / 2; k < KT; ++k) w[i][k] = first_bytes(w[i][k], p.R * 2 - k * 64 - q * 16);         // (a row ends in one of the later half)
     }
     const float scale = p.scale ? p.scale[e] : 1.0f;
     const int col = n0 + lane % LR * V, have = p.N - col;

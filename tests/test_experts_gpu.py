@@ -605,6 +605,17 @@ def test_adapters_of_large_and_small_values(x_type, more):
     G.assert_close(G.host(y.rows()), ref, bound, "f32", "large and small")
 
 
+@pytest.mark.parametrize("x_type,y_type", PAIRS[1:])
+@pytest.mark.parametrize("counts", [[3, 0, 30], [1500, 0, 70]])
+@pytest.mark.parametrize("R", [1, 9, 31, 65, 66, 82, 95, 96, 97, 127, 129, 161, 170, 191, 193, 223, 224, 225])
+def test_adapters_ignore_what_lies_behind_the_ends_of_rows(R, counts, x_type, y_type):
+    """NaN behind each row's end (adapter_rows), up to the next sixteen bytes and in the ranks that a form rounds R up to."""
+    for kw in (dict(), dict(odd=True, in_place=True)):
+        y, ref, bound = run_adapters(counts, 2, 72, 40, R, x_type, y_type, R, **kw)
+        G.assert_close(G.host(y.rows()), ref, bound, y_type, kw)
+        y.check_guard()
+
+
 @pytest.mark.parametrize("n,R", [(40, 8), (1600, 40)])
 def test_adapters_keep_what_is_not_finite_in_its_row(n, R):
     x, a, b = torch.randn(n, 64, device="cuda").bfloat16(), torch.randn(2, R, 64, device="cuda").bfloat16(), torch.randn(2, 100, R, device="cuda").bfloat16()
