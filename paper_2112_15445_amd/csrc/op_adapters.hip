@@ -126,7 +126,8 @@ template <int XT, int RN, int RT, int WR, int KW> __global__ __launch_bounds__(W
     }
 }
 
-// f as the sum of TERMS 16-bit numbers, the largest first.
+// f as the sum of TERMS 16-bit numbers, the largest first.  (A bf16 of what lies above the largest one of them is that one, and the rest the next term's: rounded to
+// an infinity it would leave another one, and their sum is a NaN.)
 template <int XT, int TERMS, int N, class V> __device__ __forceinline__ void split_terms(const float* f, V (&out)[TERMS])
 {
     float rest[N];
@@ -136,8 +137,10 @@ template <int XT, int TERMS, int N, class V> __device__ __forceinline__ void spl
     for (int t = 0; t < TERMS; ++t)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            out[t][i] = (Elem<XT>)rest[i];
-            rest[i] = fabsf(rest[i]) < INFINITY ? rest[i] - (float)out[t][i] : 0.0f;
+            constexpr float kMost = 0x1.fep+127f;
+            const bool finite = fabsf(rest[i]) < INFINITY;
+            out[t][i] = (Elem<XT>)(XT == SC_ELEM_BF16 && t == 0 && finite ? __builtin_amdgcn_fmed3f(rest[i], -kMost, kMost) : rest[i]);
+            rest[i] = finite ? rest[i] - (float)out[t][i] : 0.0f;
         }
 }
 

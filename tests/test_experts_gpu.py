@@ -616,6 +616,27 @@ def test_adapters_ignore_what_lies_behind_the_ends_of_rows(R, counts, x_type, y_
         y.check_guard()
 
 
+@pytest.mark.parametrize("y_type", ["bf16", "f32"])
+@pytest.mark.parametrize("n,R", [(3, 8), (40, 104), (2100, 8), (1600, 40), (1600, 248)])
+def test_adapters_of_a_first_product_near_the_end_of_the_range(n, R, y_type):
+    """Sums between the largest bf16, (2 - 2^-7) 2^127, and the largest 32-bit float: finite, and so is what they become.  Products and sums of powers of two: 24 bits of
+    the first product, of which the terms drop 2^-16 or 2^-24, times 2^-100."""
+    x, a, b = torch.zeros(n, 16, device="cuda").bfloat16(), torch.zeros(2, R, 16, device="cuda").bfloat16(), torch.zeros(2, 70, R, device="cuda").bfloat16()
+    x[:, 0], x[:, 1] = (2 - 2.0 ** -7) * 2.0 ** 127, 2.0 ** 119
+    x[::2] *= -1
+    a[:, :, 0] = 1
+    a[:, :, 1] = torch.arange(R, device="cuda") % 3 / 2
+    for r in range(R):
+        b[:, r % 70, r] = 2.0 ** -100
+    sign = torch.where(torch.arange(n, device="cuda") % 2 == 0, -1.0, 1.0)[:, None].double()
+    got = B.adapters_torch(torch.zeros(n, 70, device="cuda", dtype=T[y_type]), x, a, b, torch.tensor([0, n // 3, n], dtype=torch.int32, device="cuda"))
+    h = (2 - 2.0 ** -7) * 2.0 ** 127 + a[0, :, 1].double() * 2.0 ** 119
+    want = sign * (h[None] @ b[0].double().t())
+    # terms, the sum of up to four values in 32 bits, the result's own rounding
+    bound = want.abs() * ((2.0 ** -16 + 2.0 ** -8 if y_type == "bf16" else 2.0 ** -23) + 8 * 2.0 ** -24)
+    assert bool(got.isfinite().all()) and bool(((got.double() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("n,R", [(40, 8), (1600, 40)])
 def test_adapters_keep_what_is_not_finite_in_its_row(n, R):
     x, a, b = torch.randn(n, 64, device="cuda").bfloat16(), torch.randn(2, R, 64, device="cuda").bfloat16(), torch.randn(2, 100, R, device="cuda").bfloat16()
