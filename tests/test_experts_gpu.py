@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_experts_host as H
 import test_operators_gpu as G
 from oracle import experts as X
 from paper_2112_15445_amd import binding as B
@@ -635,6 +636,18 @@ def test_adapters_of_a_first_product_near_the_end_of_the_range(n, R, y_type):
     # terms, the sum of up to four values in 32 bits, the result's own rounding
     bound = want.abs() * ((2.0 ** -16 + 2.0 ** -8 if y_type == "bf16" else 2.0 ** -23) + 8 * 2.0 ** -24)
     assert bool(got.isfinite().all()) and bool(((got.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("x_type,y_type", sorted(H.TERMS_KEPT))
+@pytest.mark.parametrize("n,R", [(50, 16), (50, 24), (50, 56), (50, 120), (50, 248), (2100, 16), (2100, 24), (1100, 56), (1100, 120), (1100, 248)])
+def test_adapters_first_product_keeps_its_bits(n, R, x_type, y_type):
+    """A first product that is exact in 32 bits goes into the second one off by no more than is stated, 2^-24 (three bf16), 2^-16 (two), 2^-22 of the row's
+    largest (two f16); nothing else rounds but the result."""
+    x, a, b, scale, base, want, size = H.products_of_24_bits(n, R, 272, y_type)
+    assert B.Adapters(n, 272, 16, R, 1, x_type=T[x_type], y_type=T[y_type]).launch()["form"] == ("adapters few" if n == 50 else "adapters many")
+    xd, ad, bd = dev(x, T[x_type]), dev(a[None], T[x_type]), dev(b[None], T[x_type])
+    got = B.adapters_torch(dev(base, T[y_type]), xd, ad, bd, torch.tensor([0, n], dtype=torch.int32, device="cuda"), scale=torch.full((1,), scale, device="cuda"))
+    G.assert_close(G.host(got), want, H.TERMS_KEPT[x_type, y_type][1] * size, y_type, "terms")
 
 
 @pytest.mark.parametrize("n,R", [(40, 8), (1600, 40)])

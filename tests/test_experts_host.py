@@ -206,3 +206,48 @@ def test_oracle_combine_and_its_gradients_against_torch():
     (y * dy).sum().backward()
     dx, _, dw, _ = X.combine_backward(dy.numpy(), x.detach().numpy(), position, w.detach().numpy())
     assert np.allclose(dx, x.grad.numpy()) and np.allclose(dw, w.grad.numpy())
+
+
+# -- how many 16-bit numbers carry the adapters' first product ------------------------------------------------
+
+TERMS_KEPT = {("bf16", "bf16"): (2, 2.0 ** -16), ("f16", "f16"): (2, 2.0 ** -22), ("f16", "f32"): (2, 2.0 ** -22), ("bf16", "f32"): (3, 2.0 ** -24)}
+
+
+def products_of_24_bits(n, R, N, y_type, seed=0):
+    """(x [n, 16], a [R, 16], b [N, R], scale, base [n, N], what base + scale (x a^T) b^T is, the same of magnitudes of the first product alone): all of it 16-bit
+    numbers, the first product whole numbers of up to 24 bits times a power of two, so exact in 32 bits however it is summed; each column has one rank, a power of two.  With
+    16-bit results base takes the leading bits away, so that the last ones are seen."""
+    rng = np.random.default_rng(seed)
+    x, a, b = np.zeros((n, 16)), np.zeros((R, 16)), np.zeros((N, R))
+    x[:, [1, 6, 12]] = rng.integers(0, 256, size=(n, 3)) * rng.choice([-1, 1], size=(n, 1))
+    a[:, [1, 6, 12]] = 2.0 ** np.array([15, 7, -1]) * 2.0 ** -(np.arange(R)[:, None] % 3)
+    b[np.arange(N), (7 * np.arange(N) + 3) % R] = 2.0 ** (np.arange(N) % 2)
+    scale, h = 2.0 ** -12, x @ a.T
+    added = scale * (h @ b.T)
+    base = np.zeros((n, N)) if y_type == "f32" else -rounded(added, y_type)
+    return x, a, b, scale, base, base + added, scale * (np.abs(h).max(1, keepdims=True) @ np.abs(b).sum(1)[None])
+
+
+def rounded(v, kind):
+    return torch.from_numpy(np.asarray(v)).float().to({"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[kind]).double().numpy()
+
+
+@pytest.mark.parametrize("x_type,y_type", sorted(TERMS_KEPT))
+@pytest.mark.parametrize("R", [16, 250])
+def test_a_term_less_is_seen(R, x_type, y_type):
+    """What the GPU's results are compared with (test_adapters_first_product_keeps_its_bits) holds with all terms of the first product, and not with one less."""
+    x, a, b, scale, base, want, size = products_of_24_bits(60, R, 272, y_type)
+    for v, kind in ((x, x_type), (a, x_type), (b, x_type), (base, y_type)):
+        assert np.array_equal(rounded(v, kind), v)
+    h = x @ a.T
+    assert np.array_equal(h.astype(np.float32), h)
+    up = 2.0 ** (14 - np.frexp(np.abs(h).max(1, keepdims=True))[1]) if x_type == "f16" else 1.0
+    terms, off = TERMS_KEPT[x_type, y_type]
+    for n in (terms, terms - 1):
+        rest, kept = h * up, 0.0
+        for _ in range(n):
+            kept, rest = kept + rounded(rest, x_type), rest - rounded(rest, x_type)
+        got = rounded(base + scale * ((kept / up) @ b.T), y_type)
+        step = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[y_type]
+        over = (np.abs(got - want) - (off * size + step * (np.abs(want) + off * size))).max()
+        assert over <= 0 if n == terms else over > 0
