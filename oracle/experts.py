@@ -47,12 +47,18 @@ def route(x, top, kind="softmax", normalize=False, factor=1.0, bias=None):
     c = np.where(np.isnan(c) | np.isnan(x) | (x == -np.inf), -np.inf, c)
     ids = np.argsort(-c, axis=1, kind="stable")[:, :top].astype(np.int32)
     ids = np.where(np.take_along_axis(c, ids, 1) > -np.inf, ids, -1)
-    w = np.zeros((T, top))
-    for t in range(T):
+    return ids, *weights(x, ids, kind, normalize, factor)
+
+
+def weights(x, ids, kind="softmax", normalize=False, factor=1.0):
+    """(weights of these ids, bound): see route."""
+    x = np.asarray(x, np.float64)
+    s, w = scores(x, kind), np.zeros(ids.shape)
+    for t in range(len(x)):
         live = ids[t] >= 0
         if live.any():
             w[t, live] = factor * (shares(x[t, ids[t, live]], kind) if normalize else s[t, ids[t, live]])
-    return ids, w, np.abs(w) * U * (2 * spread(x) + 90) + TINY
+    return w, np.abs(w) * U * (2 * spread(x) + 90) + TINY
 
 
 def route_backward(x, ids, dweights, kind="softmax", normalize=False, factor=1.0):

@@ -164,11 +164,14 @@ template <int L, class T, int V> __device__ __forceinline__ T choose(T (&key)[V]
     return slot;
 }
 
-// exp of |x| <= 700 (else of that) and the reciprocal in 64 bits, off by some 2^-50: x = (n + r) ln 2 with |r| <= 1/2, the series of exp(r ln 2) up to the twelfth power, whose
-// rest is 2e-16; the hardware's reciprocal with two steps of Newton's.
+// exp of x <= 0 and the reciprocal of 1 and more in 64 bits, off by some 2^-51: x log2(e) = n + r with |r| <= 1/2, where r takes the product unrounded and the constant's
+// lower half (from the rounded product it would be off by |x| 2^-53); the series of exp(r ln 2) up to the twelfth power, whose rest is 2e-16; 0 below e^-745, what 64 bits
+// hold.  The hardware's reciprocal with two steps of Newton's.
 __device__ __forceinline__ double exp64(double x)
 {
-    const double t = fmin(fmax(x, -700.0), 700.0) * 0x1.71547652b82fep+0, n = rint(t), r = (t - n) * 0x1.62e42fefa39efp-1;
+    constexpr double kLog2e = 0x1.71547652b82fep+0, kLog2eLow = 0x1.777d0ffda0d24p-56;
+    x = fmax(x, -746.0);
+    const double n = rint(x * kLog2e), r = fma(x, kLog2eLow, fma(x, kLog2e, -n)) * 0x1.62e42fefa39efp-1;
     double p = 1.0 / 479001600.0;
     constexpr double k[] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
@@ -246,7 +249,10 @@ template <int XT, bool BIAS, int L, int V> __global__ __launch_bounds__(256) voi
             for (int v = 0; v < V; ++v) c[v] *= inv;
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) c[v] = reciprocal64(1.0 + exp64(-(double)x[v]));
+            for (int v = 0; v < V; ++v) {
+                const double e = exp64(-fabs((double)x[v])), r = reciprocal64(1.0 + e);
+                c[v] = x[v] < 0.0f ? e * r : r;
+            }
         }
         uint64_t key[V];
 #pragma unroll

@@ -84,6 +84,44 @@ def test_route(T_, E, top, pad, lead, x_type, kind):
                 G.assert_close(w, ref, bound, "f32", what)
 
 
+def assert_chosen(ids, w, x, bias, score, normalize, factor):
+    """What the header says of a choice with a bias: sums of score and bias whose first forty bits are alike may come in any order, and so may those that the score's own
+    rounding (2^-51 of it) brings there; the numbers next to zero are 2^-1074 apart, twelve bits of them 2^-1062.  The weights are those of the ids that were chosen."""
+    ref_ids = X.route(x, ids.shape[1], score, normalize, factor, bias)[0]
+    s = X.scores(x, score)
+    c = s + np.asarray(bias, np.float64)
+    for t, j in np.argwhere(ids != ref_ids):
+        g, r = ids[t, j], ref_ids[t, j]
+        assert g >= 0 and abs(c[t, g] - c[t, r]) <= 2.0 ** -40 * max(abs(c[t, g]), abs(c[t, r])) + 2.0 ** -50 * max(s[t, g], s[t, r]) + 2.0 ** -1061, (t, j, ids[t], ref_ids[t])
+    assert all(len(set(row[row >= 0])) == (row >= 0).sum() for row in ids)
+    ref, bound = X.weights(x, ids, score, normalize, factor)
+    G.assert_close(w, ref, bound, "f32", (score, normalize))
+
+
+@pytest.mark.parametrize("x_type", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T_,E,top,pad,lead", ROUTES)
+@pytest.mark.parametrize("kind", ["plain", "ties", "out", "wide"])
+def test_route_with_a_bias(T_, E, top, pad, lead, x_type, kind):
+    """Every kind of logits with a bias, and with one that is zero everywhere, where scores far below the largest still have an order."""
+    x = logits(T_, E, T_ + 7 * E, kind)
+    for bias in ((0.3 * np.random.default_rng(E).normal(size=E)).astype(np.float32), np.zeros(E, np.float32)):
+        for score in ("softmax", "sigmoid"):
+            for normalize in (False, True):
+                xd, ids, w = run_route(x, top, x_type, pad, lead, bias, score=score, normalize=normalize, factor=2.5)
+                assert_chosen(ids, w, G.host(xd), bias, score, normalize, 2.5)
+
+
+@pytest.mark.parametrize("E,top", [(16, 16), (100, 16), (200, 15), (40, 20), (500, 30), (1000, 17), (3000, 64)])
+def test_route_with_a_bias_orders_the_least_scores(E, top):
+    """Scores that only 64 bits hold, e^-690 to e^-729, have their order, and those that are zero come behind them by rising number."""
+    rng = np.random.default_rng(E)
+    far = np.concatenate([[0], -690.0 - 3 * np.arange(14), -1000.0 - np.arange(E)])[:E]
+    x = np.stack([far[rng.permutation(E)] for _ in range(9)])
+    for score in ("softmax", "sigmoid"):
+        ids = run_route(x, top, "f32", bias=np.zeros(E, np.float32), score=score)[1]
+        assert np.array_equal(ids, X.route(x, top, score, bias=np.zeros(E))[0]), score
+
+
 @pytest.mark.parametrize("x_type", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("T_,E,top,pad,lead", ROUTES)
 @pytest.mark.parametrize("kind", ["plain", "out", "wide"])
