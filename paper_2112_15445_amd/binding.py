@@ -701,10 +701,12 @@ def _rows(t, what: str):
     return t
 
 
-def _forward_only(*tensors):
+def _forward_only(*tensors, gradient: str = ""):
+    """`gradient`: the call that takes the gradient of this one, which autograd does not make."""
     import torch
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError("the operators have no gradient: call them under torch.no_grad(), or on detached tensors")
+        what = f"autograd does not see this operator, whose gradient is {gradient}" if gradient else "the operators have no gradient"
+        raise ValueError(f"{what}: call {'both' if gradient else 'them'} under torch.no_grad(), or on detached tensors")
 
 
 def _params(t, n: int, like, what: str):
@@ -828,7 +830,7 @@ def route_experts_torch(logits, top: int, score: str = "softmax", normalize: boo
     import torch
     if _rows(logits, "logits").dim() != 2:
         raise ValueError(f"logits: a matrix, not {list(logits.shape)}")
-    _forward_only(logits, bias)
+    _forward_only(logits, bias, gradient="route_experts_backward_torch")
     T, E = logits.shape
     ids = torch.empty(T, top, dtype=torch.int32, device=logits.device)
     weights = torch.empty(T, top, dtype=torch.float32, device=logits.device)
@@ -873,7 +875,7 @@ def gather_rows_torch(x, index):
     import torch
     if _rows(x, "x").dim() != 2:
         raise ValueError(f"x: a matrix, not {list(x.shape)}")
-    _forward_only(x)
+    _forward_only(x, gradient="combine_rows_torch")
     _integers(index, x, "index")
     M, (rows, C) = index.numel(), x.shape
     y = empty_codes(M, C, device=x.device) if x.dtype == torch.float8_e4m3fn else torch.empty(M, C, dtype=x.dtype, device=x.device)
@@ -888,7 +890,7 @@ def combine_rows_torch(x, position, weights=None, residual=None, dtype=None):
     import torch
     if _rows(x, "x").dim() != 2 or position.dim() != 2:
         raise ValueError(f"x [rows, C] and position [T, top], not {list(x.shape)} and {list(position.shape)}")
-    _forward_only(x, weights, residual)
+    _forward_only(x, weights, residual, gradient="combine_rows_backward_torch")
     (rows, C), (T, top) = x.shape, position.shape
     _table(position, (T, top), torch.int32, x, "position")
     if weights is not None:

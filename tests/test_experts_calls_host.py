@@ -152,3 +152,15 @@ def test_shapes_that_do_not_belong_together_are_refused(calls):
         with pytest.raises(ValueError):
             call()
         assert not calls, i
+
+
+def test_the_refusal_of_a_gradient_names_the_call_that_takes_it(calls):
+    for name, arg, back in (("route", "logits", "route_experts_backward_torch"), ("route", "bias", "route_experts_backward_torch"), ("gather", "x", "combine_rows_torch"),
+                            ("combine", "x", "combine_rows_backward_torch"), ("combine", "weights", "combine_rows_backward_torch"), ("combine", "residual", "combine_rows_backward_torch")):
+        with pytest.raises(ValueError, match=f"gradient is {back}"):
+            one_of_each(change=lambda n, t, arg=arg: t.requires_grad_() if n == arg else t)[name]()
+        assert callable(getattr(B, back))
+    for name, arg in (("route back", "logits"), ("combine back", "dy"), ("adapters", "x")):
+        with pytest.raises(ValueError, match="no gradient"):
+            one_of_each(change=lambda n, t, arg=arg: t.requires_grad_() if n == arg else t)[name]()
+    assert not calls
