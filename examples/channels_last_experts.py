@@ -5,7 +5,7 @@
     two experts a position, rows sorted by expert
     codes x first layer of the experts, SiLU        rows picked from the positions by an index
     -> codes, x second layer of the experts         quantised, grouped again
-    + x                                             rows back to their positions, weighted with the scores
+    + x                                             32-bit rows back to their positions, weighted with the scores; rounded once
 
     python examples/channels_last_experts.py [samples] [height] [width] [channels]
 
@@ -45,9 +45,9 @@ class Block:
         offsets, index, position = B.sort_by_expert_torch(ids, self.first.shape[0])
         h = B.matmul_grouped_torch(q, self.first_q[0], offsets, scale, self.first_q[1], index=index, bias=self.bias, act="silu")
         hq, h_scale = B.quantize_blocks_torch(h)
-        y = B.matmul_grouped_torch(hq, self.second_q[0], offsets, h_scale, self.second_q[1], dtype=x.dtype)
-        out = B.combine_rows_torch(y, position, weights, residual=x.view(-1, x.shape[-1]))
-        return out.view(x.shape), (weights, offsets, index, position)
+        y = B.matmul_grouped_torch(hq, self.second_q[0], offsets, h_scale, self.second_q[1], dtype=torch.float32)
+        out = B.combine_rows_torch(y, position, weights, residual=x.view(-1, x.shape[-1]).float())
+        return out.view(x.shape).to(x.dtype), (weights, offsets, index, position)
 
     def reference(self, x, chosen):
         """The same in 32 bits, with the experts that were chosen."""

@@ -892,6 +892,26 @@ def test_experts_in_16_bits_as_they_are_served():
         torch.zeros(1000, device="cuda").sum().item()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_the_example_rounds_once(dtype):
+    """The block of examples/channels_last_experts.py adds the experts' 32-bit rows to its input in 32 bits and rounds the sum, nothing before."""
+    import importlib.util
+    import os
+    spec = importlib.util.spec_from_file_location("example", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "channels_last_experts.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    block = m.Block(192)
+    x = torch.randn(2, 63, 192, device="cuda").to(T[dtype])
+    out, (weights, offsets, index, position) = block.forward(x)
+    q, scale = B.group_norm_torch(x, block.groups, block.gamma, block.beta, act="silu", codes=True)
+    h = B.matmul_grouped_torch(q, block.first_q[0], offsets, scale, block.first_q[1], index=index, bias=block.bias, act="silu")
+    hq, h_scale = B.quantize_blocks_torch(h)
+    y = B.matmul_grouped_torch(hq, block.second_q[0], offsets, h_scale, block.second_q[1], dtype=torch.float32)
+    ref, bound = X.combine(G.host(y), position.cpu().numpy(), G.host(weights), G.host(x).reshape(-1, 192))
+    assert out.dtype == x.dtype
+    G.assert_close(G.host(out).reshape(-1, 192), ref, bound, dtype, "block")
+
+
 def test_adapters_beside_a_shared_projection():
     """A projection for all tokens (the products by expert with one expert), the adapters of four requests on top, some tokens without one."""
     g = torch.Generator(device="cuda").manual_seed(6)
