@@ -153,6 +153,29 @@ def test_names_of_the_forms_match_the_header(tmp_path):
             op.launch()
 
 
+def test_expert_kernels_spill_at_most_four_registers():
+    """No scratch memory but in the adapters' second launch for few rows, 32-bit results and ranks of 65 to 128: four registers of it (f16), two (bf16).  Without
+    that cap of 256 registers, one wave a SIMD, they take 32.7 us for 28.7 (768 rows of rank 128)."""
+    import re
+
+    import test_kernel_resources as R
+    with open(B.LIB_PATH, "rb") as f:
+        data = f.read()
+    count = {}
+    for name, k in {k[".name"]: k for elf in R._code_objects(data) for k in R._kernels(elf)}.items():
+        m = re.search(r"(route_pick|route_gradient|sort_count|sort_scan|sort_place|sort_nothing|gather_rows|combine_rows|combine_gradient|adapters_down|adapters_up|adapters_down_wide|adapters_up_wide)_kernel(I|E)", name)
+        if not m:
+            continue
+        kind = m.group(1)
+        count[kind] = count.get(kind, 0) + 1
+        capped = re.search(r"adapters_up_kernelILi[12]ELi0ELi4E", name)
+        assert k[".vgpr_spill_count"] <= (4 if capped else 0) and k[".private_segment_fixed_size"] <= (20 if capped else 0), name
+    # router: 3 types, 5 sizes, with a bias or without (gradient: of whole rows or not); sort: two numbers of experts, one workgroup or chunks; rows back: 5 pairs of types
+    # (gradients: 3 lengths, 3 choices of what is taken); adapters: 4 pairs; first launch 3 ranks or, many rows, 10 forms; second 4 ranks
+    assert count == {"route_pick": 30, "route_gradient": 30, "sort_count": 1, "sort_scan": 1, "sort_place": 4, "sort_nothing": 1, "gather_rows": 1, "combine_rows": 5, "combine_gradient": 45,
+                     "adapters_down": 2 * 3, "adapters_down_wide": 4 * 10, "adapters_up": 4 * 4, "adapters_up_wide": 4 * 4}
+
+
 # -- the oracle's own definitions ------------------------------------------------------------------
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
