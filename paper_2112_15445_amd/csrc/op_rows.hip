@@ -1,7 +1,11 @@
 // Rows out to their places and back (sparse_conv_gather_rows, sparse_conv_combine_rows and its gradients).
 //
-// All of them are bound by memory: sixteen bytes a lane (of x), lanes along a row, several rows under way at once.  What is read or written once goes past
-// the caches (8192 x 2 rows of 4096 bf16 back with a residual 52 -> 47 us, 5.7 TB/s; 4096 x 8 rows of 2048 back 35 -> 29, out 39 -> 36).
+// All of them are bound by memory: sixteen bytes a lane (of x), lanes along a row, several rows under way at once.  What is read once goes past
+// the caches, and so do results of more than 32 MiB (8192 x 2 rows of 4096 bf16 back with a residual 52 -> 47 us, 5.7 TB/s; 4096 x 8 rows of 2048 back 35 -> 29, out 39 -> 36).
+// Smaller ones stay in them for the call behind (us, through the caches and past them; rows of bf16, out alone and with a product by expert of 1024 columns behind: 8 x 2 of
+// 2048 3.4 and 3.5, 11.2 and 12.2; 256 x 2 3.6 and 3.6, 12.8 and 15.1; 2048 x 2 6.1 and 5.9, 38 and 42; back alone and with a quantiser behind: 8192 of 2048 24.6 and 25.5, 35 and
+// 38; 4096 of 4096 25.9 and 25.2, 36.6 and 37.0).  Of larger ones less is left there than it costs: out with a quantiser 64 MiB 22 and 20, 39 and 41, 128 MiB 43 and 39, 77 and 75;
+// back 64 MiB 54 and 46, 71 and 72.  (A product that reads its rows again for every tile of columns would have 64 MiB there, 70 and 78.)
 #include "op_common.h"
 
 #include <algorithm>
@@ -11,6 +15,7 @@ namespace sc {
 namespace {
 
 constexpr int kRowThreads = 256;
+constexpr int64_t kKept = 32 << 20;          // bytes of a result that stay in the caches
 
 struct GatherArgs {
     const uint8_t* x;
@@ -32,11 +37,13 @@ __device__ __forceinline__ v4i chunk_of(const uint8_t* row, int have)
     }
     return v;
 }
-__device__ __forceinline__ void put_chunk(uint8_t* row, v4i v, int have)
+template <bool PAST> __device__ __forceinline__ void put_chunk(uint8_t* row, v4i v, int have)
 {
     typedef int any4i __attribute__((ext_vector_type(4), aligned(1)));
-    if (have >= 16) __builtin_nontemporal_store(v, reinterpret_cast<any4i*>(row));
-    else {
+    if (have >= 16) {
+        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<any4i*>(row));
+        else *reinterpret_cast<any4i*>(row) = v;
+    } else {
         uint8_t b[16];
         __builtin_memcpy(b, &v, 16);
 #pragma unroll
@@ -46,7 +53,7 @@ __device__ __forceinline__ void put_chunk(uint8_t* row, v4i v, int have)
 }
 
 // U rows a lane under way at once.
-template <int U> __global__ __launch_bounds__(kRowThreads) void gather_rows_kernel(GatherArgs a)
+template <int U, bool PAST> __global__ __launch_bounds__(kRowThreads) void gather_rows_kernel(GatherArgs a)
 {
     const int per = kRowThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1);
     const int64_t first = (int64_t)blockIdx.x * (per * U) + threadIdx.x / a.lanes;
@@ -63,7 +70,7 @@ template <int U> __global__ __launch_bounds__(kRowThreads) void gather_rows_kern
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (first + u * per < a.M) put_chunk(a.y + (first + u * per) * a.y_row + c * 16, v[u], have);
+            if (first + u * per < a.M) put_chunk<PAST>(a.y + (first + u * per) * a.y_row + c * 16, v[u], have);
     }
 }
 
@@ -80,9 +87,16 @@ struct CombineArgs {
     int64_t x_row, y_row, residual_row, dx_row;
 };
 
+// V values that are whole, past the caches or through them.  (The choice is the kernel's: of two stores behind a branch the compiler makes one, through the caches.)
+template <int ET, bool PAST, int V> __device__ __forceinline__ void put_values(Elem<ET>* y, const float (&f)[V])
+{
+    if constexpr (PAST) store_once<ET, V>(y, f);
+    else store_values<ET, V>(y, V, f);
+}
+
 // y[t] = residual[t] + sum over j of weights[t,j] x[position[t,j]], in the order of j, in 32 bits; kSlots rows are read together.
 constexpr int kSlots = 4;
-template <int XT, int YT> __global__ __launch_bounds__(kRowThreads) void combine_rows_kernel(CombineArgs a)
+template <int XT, int YT, bool PAST> __global__ __launch_bounds__(kRowThreads) void combine_rows_kernel(CombineArgs a)
 {
     constexpr int V = kVec<XT>;
     const int per = kRowThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1);
@@ -122,7 +136,7 @@ template <int XT, int YT> __global__ __launch_bounds__(kRowThreads) void combine
             }
         }
         Elem<YT>* y = static_cast<Elem<YT>*>(a.y) + t * a.y_row + c;
-        if constexpr (WHOLE) store_once<YT, V>(y, sum);
+        if constexpr (WHOLE) put_values<YT, PAST>(y, sum);
         else store_values<YT, V>(y, have, sum);
     };
     int c = lane * V;
@@ -132,7 +146,7 @@ template <int XT, int YT> __global__ __launch_bounds__(kRowThreads) void combine
 
 // dx[position[t,j]] = weights[t,j] dy[t], dweights[t,j] = sum of dy[t] x[position[t,j]]: L lanes a token (16 or 64, or the workgroup's four waves), kSlots slots at a
 // time, whose rows are read together (a slot without a row reads row 0 and drops it, so that no load waits behind a branch).
-template <int XT, int YT, int L, bool DX, bool DW> __global__ __launch_bounds__(kRowThreads) void combine_gradient_kernel(CombineArgs a)
+template <int XT, int YT, int L, bool DX, bool DW, bool PAST> __global__ __launch_bounds__(kRowThreads) void combine_gradient_kernel(CombineArgs a)
 {
     constexpr int V = kVec<XT>, W = kRowThreads / 64;
     __shared__ float part[L == kRowThreads ? W : 1][L == kRowThreads ? 64 : 1];
@@ -175,7 +189,7 @@ template <int XT, int YT, int L, bool DX, bool DW> __global__ __launch_bounds__(
                     if constexpr (DX) {
 #pragma unroll
                         for (int i = 0; i < V; ++i) f[i] = g[i] * w[j];
-                        if (real[j] && t < a.T) store_once<XT, V>(dx[j] + c, f);
+                        if (real[j] && t < a.T) put_values<XT, PAST>(dx[j] + c, f);
                     }
                 }
             }
@@ -261,25 +275,29 @@ CombineArgs args(const sc_combine_rows_t* d, const int32_t* position, const floa
 template <int XT, int YT> sc_status_t launch_combine(CombineArgs a, hipStream_t s)
 {
     a.lanes = lanes_of(ceil_div(a.C, kVec<XT>));
-    combine_rows_kernel<XT, YT><<<(unsigned)ceil_div(a.T, kRowThreads / a.lanes), kRowThreads, 0, s>>>(a);
+    const unsigned grid = (unsigned)ceil_div(a.T, kRowThreads / a.lanes);
+    if ((int64_t)a.T * a.C * (int64_t)sizeof(Elem<YT>) > kKept) combine_rows_kernel<XT, YT, true><<<grid, kRowThreads, 0, s>>>(a);
+    else combine_rows_kernel<XT, YT, false><<<grid, kRowThreads, 0, s>>>(a);
     return launched();
 }
 
 // A wave a token up to 64 chunks of a row, and up to 192 with many tokens, where the lanes of a workgroup that have no chunk cost more than the turns of a wave
 // (us: 16384 x 2 rows of 128 chunks 42 with 256 lanes and 29 with 64, of 192 chunks 50 and 42, 8192 x 2 of 256 chunks 31 and 33; 64 x 8 of 128 chunks 5.1 and 6.6).
-template <int XT, int YT, bool DX, bool DW> sc_status_t launch_gradient_of(const CombineArgs& a, hipStream_t s)
+template <int XT, int YT, bool DX, bool DW, bool PAST> sc_status_t launch_gradient_of(const CombineArgs& a, hipStream_t s)
 {
     const int64_t chunks = ceil_div(a.C, kVec<XT>);
-    if (chunks <= 16) combine_gradient_kernel<XT, YT, 16, DX, DW><<<(unsigned)ceil_div(a.T, 16), kRowThreads, 0, s>>>(a);
-    else if (chunks <= 64 || (chunks <= 192 && a.T >= 1024)) combine_gradient_kernel<XT, YT, 64, DX, DW><<<(unsigned)ceil_div(a.T, 4), kRowThreads, 0, s>>>(a);
-    else combine_gradient_kernel<XT, YT, kRowThreads, DX, DW><<<(unsigned)a.T, kRowThreads, 0, s>>>(a);
+    if (chunks <= 16) combine_gradient_kernel<XT, YT, 16, DX, DW, PAST><<<(unsigned)ceil_div(a.T, 16), kRowThreads, 0, s>>>(a);
+    else if (chunks <= 64 || (chunks <= 192 && a.T >= 1024)) combine_gradient_kernel<XT, YT, 64, DX, DW, PAST><<<(unsigned)ceil_div(a.T, 4), kRowThreads, 0, s>>>(a);
+    else combine_gradient_kernel<XT, YT, kRowThreads, DX, DW, PAST><<<(unsigned)a.T, kRowThreads, 0, s>>>(a);
     return launched();
 }
 
 template <int XT, int YT> sc_status_t launch_gradient(const CombineArgs& a, hipStream_t s)
 {
-    if (!a.dweights) return launch_gradient_of<XT, YT, true, false>(a, s);
-    return a.dx ? launch_gradient_of<XT, YT, true, true>(a, s) : launch_gradient_of<XT, YT, false, true>(a, s);
+    if (!a.dx) return launch_gradient_of<XT, YT, false, true, false>(a, s);
+    const bool past = std::min<int64_t>(a.rows, (int64_t)a.T * a.top) * a.C * (int64_t)sizeof(Elem<XT>) > kKept;
+    if (a.dweights) return past ? launch_gradient_of<XT, YT, true, true, true>(a, s) : launch_gradient_of<XT, YT, true, true, false>(a, s);
+    return past ? launch_gradient_of<XT, YT, true, false, true>(a, s) : launch_gradient_of<XT, YT, true, false, false>(a, s);
 }
 
 }  // namespace
@@ -302,7 +320,10 @@ extern "C" sc_status_t sparse_conv_gather_rows(const sc_gather_rows_t* d, const 
     a.M = d->M; a.rows = d->rows; a.bytes = d->C * e; a.chunks = (int)ceil_div(a.bytes, 16); a.lanes = lanes_of(a.chunks);
     a.x_row = d->x_row * e; a.y_row = d->y_row * e;
     constexpr int U = 2;
-    gather_rows_kernel<U><<<(unsigned)ceil_div(a.M, kRowThreads / a.lanes * U), kRowThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+    const unsigned grid = (unsigned)ceil_div(a.M, kRowThreads / a.lanes * U);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if ((int64_t)a.M * a.bytes > kKept) gather_rows_kernel<U, true><<<grid, kRowThreads, 0, s>>>(a);
+    else gather_rows_kernel<U, false><<<grid, kRowThreads, 0, s>>>(a);
     return launched();
 }
 

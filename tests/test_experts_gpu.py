@@ -559,6 +559,44 @@ def test_rows_further_than_32_bits_reach():
     assert torch.equal(far[:, :C], x.flip(0))
 
 
+@pytest.mark.parametrize("x_type,y_type", PAIRS)
+@pytest.mark.parametrize("C,pad,lead", [(2056, 0, 0), (2053, 3, 1)])
+def test_rows_of_large_results(C, pad, lead, x_type, y_type):
+    """Results of more than 32 MiB, which go past the caches, against the same in parts, which stay in them: the same bits, and nothing between the rows."""
+    size = 4 if y_type == "f32" else 2
+    T_, top, step = (33 << 20) // (C * size) + 1, 2, 1000
+    for rows, kind in ((T_, y_type), (2 * T_, x_type)):
+        assert rows * C * (4 if kind == "f32" else 2) > 32 << 20
+    g = torch.Generator(device="cuda").manual_seed(C)
+    ids = torch.randint(-1, 5, (T_, top), generator=g, device="cuda", dtype=torch.int32)
+    _, index, position = B.sort_by_expert_torch(ids, 5)
+    made = lambda M, t: torch.randn(lead + M * (C + pad), generator=g, device="cuda").to(T[t])[lead:].view(M, C + pad)[:, :C]  # noqa: E731
+    x, rows, residual, w = made(T_, x_type), made(T_ * top, x_type), made(T_, y_type), torch.rand(T_, top, generator=g, device="cuda")
+    row = C + pad
+    out = G.Out(T_ * top, C, x_type, row, lead)
+    B.RowGather(T_ * top, C, T_, x_type=T[x_type], x_row=row, y_row=row).forward(x.data_ptr(), index.data_ptr(), out.ptr, G.stream())
+    y = G.Out(T_, C, y_type, row, lead)
+    op = B.RowCombine(T_, top, C, T_ * top, x_type=T[x_type], y_type=T[y_type], x_row=row, y_row=row, residual_row=row, dx_row=row)
+    op.forward(rows.data_ptr(), position.data_ptr(), w.data_ptr(), residual.data_ptr(), y.ptr, G.stream())
+    dx, dw = G.Out(T_ * top, C, x_type, row, lead), G.Out(T_, top, "f32")
+    op.backward(residual.data_ptr(), rows.data_ptr(), position.data_ptr(), w.data_ptr(), dx.ptr, dw.ptr, G.stream())
+    torch.cuda.synchronize()
+    for t in range(0, T_ * top, step):
+        assert torch.equal(out.rows()[t:t + step], B.gather_rows_torch(x, index[t:t + step]))
+    taken = torch.zeros(T_ * top, dtype=torch.bool, device="cuda")
+    for t in range(0, T_, step):
+        p, part, some = position[t:t + step], w[t:t + step], slice(t, t + step)
+        assert torch.equal(y.rows()[some], B.combine_rows_torch(rows, p, part, residual[some], dtype=T[y_type]))
+        # (the gradient of a part of the tokens, with their own rows alone)
+        there = p[p >= 0].long()
+        own = torch.full_like(p, -1)
+        own[p >= 0] = torch.arange(len(there), device="cuda", dtype=torch.int32)
+        want = B.combine_rows_backward_torch(residual[some], rows[there], own, part)
+        assert torch.equal(dx.rows()[there], want[0]) and torch.equal(dw.rows()[some], want[1])
+        taken[there] = True
+    out.check_guard(), y.check_guard(), dw.check_guard(), dx.check_guard(written=taken.nonzero()[:, 0].tolist())
+
+
 # -- low-rank adapters ------------------------------------------------------------------------------
 
 ADAPTERS = [  # rows of each adapter, rows without one, columns, summed values, rank
