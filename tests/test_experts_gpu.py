@@ -714,6 +714,30 @@ def test_adapters_of_a_first_product_near_the_end_of_the_range(n, R, y_type):
     assert bool(got.isfinite().all()) and bool(((got.double() - want).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("x_type,y_type", PAIRS[1:])
+@pytest.mark.parametrize("counts,N,K,R", [([20], 72, 8200, 16), ([30, 9], 96, 4096, 256), ([700, 290], 2200, 264, 24), ([400, 400], 1900, 2056, 60), ([2, 0, 3], 200, 12296, 100), ([700], 2600, 1032, 200),
+                                          ([1000, 1, 899], 1100, 2056, 17), ([1, 2], 40, 20000, 33)])
+def test_adapters_of_few_rows_that_share_the_summed_dimension(counts, N, K, R, x_type, y_type):
+    """Long sums, shared by 4, 8 and 16 workgroups, and waves with 3 and 4 times 32 columns (and both)."""
+    assert B.Adapters(sum(counts), N, K, R, len(counts)).launch()["form"] == "adapters few"
+    y, ref, bound = run_adapters(counts, 3, N, K, R, x_type, y_type, K)
+    G.assert_close(G.host(y.rows()), ref, bound, y_type, "shared")
+    y.check_guard()
+
+
+@pytest.mark.parametrize("x_type", ["f16", "bf16"])
+@pytest.mark.parametrize("n,R", [(40, 8), (40, 80), (2100, 24), (1600, 200)])
+def test_adapters_keep_what_is_not_finite_in_b_in_its_column(n, R, x_type):
+    x, a, b = (torch.randn(*shape, device="cuda").to(T[x_type]) for shape in ((n, 64), (2, R, 64), (2, 100, R)))
+    off = torch.tensor([0, n // 2, n], dtype=torch.int32, device="cuda")
+    want = B.adapters_torch(torch.zeros(n, 100, device="cuda"), x, a, b, off)
+    b[0, 7, R - 1], b[0, 40, 0], b[1, 99, R // 2] = float("nan"), float("inf"), float("-inf")
+    got = B.adapters_torch(torch.zeros(n, 100, device="cuda"), x, a, b, off)
+    assert not got[:n // 2, [7, 40]].isfinite().any() and not got[n // 2:, 99].isfinite().any()
+    got[:n // 2, [7, 40]], got[n // 2:, 99] = want[:n // 2, [7, 40]], want[n // 2:, 99]
+    assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("x_type,y_type", sorted(H.TERMS_KEPT))
 @pytest.mark.parametrize("n,R", [(50, 16), (50, 24), (50, 56), (50, 120), (50, 248), (2100, 16), (2100, 24), (1100, 56), (1100, 120), (1100, 248)])
 def test_adapters_first_product_keeps_its_bits(n, R, x_type, y_type):
