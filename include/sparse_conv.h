@@ -607,7 +607,7 @@ typedef enum {
     SC_FORM_SORT_ONE = 10,           /* one workgroup */
     SC_FORM_SORT_CHUNKS = 11,        /* three launches */
     SC_FORM_ADAPTERS_FEW = 12,       /* 16 rows a workgroup, the summed dimension shared by several */
-    SC_FORM_ADAPTERS_MANY = 13       /* 64 rows a workgroup, then 128 */
+    SC_FORM_ADAPTERS_MANY = 13       /* 32 or 64 rows a workgroup, then 128 */
 } sc_expert_form_t;
 
 typedef struct {
@@ -706,12 +706,12 @@ typedef struct {
 } sc_gather_rows_t;
 
 /*   x, y device, element-aligned      index [M] device i32
- * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (type, alignment), SC_ERR_RANGE (M > 2^23, C > 2^28, distances of 2^32 or more),
- * SC_ERR_HIP. */
+ * Errors: SC_ERR_NULL, SC_ERR_SHAPE, SC_ERR_UNSUPPORTED (type, alignment), SC_ERR_RANGE (M > 2^23: more rows take several calls, each with its part of
+ * index and y; C > 2^28, distances of 2^32 or more), SC_ERR_HIP. */
 sc_status_t sparse_conv_gather_rows(const sc_gather_rows_t* d, const void* x, const int32_t* index, void* y, void* stream);
 
 /* Rows back to their tokens: y[t,:] = residual[t,:] + sum_j weights[t,j] x[position[t,j],:], summed in 32 bits in the order of the slots, y
- * rounded once.  A slot whose position lies outside 0 .. rows - 1 adds nothing, whatever its weight. */
+ * rounded once.  A slot whose position lies outside 0 .. rows - 1 adds nothing, whatever its weight.  Rows of 32 bits need y and residual of 32 bits. */
 typedef struct {
     int32_t T, top, C;           /* T >= 0, 1 <= top <= 64, C >= 1 */
     int32_t rows;                /* rows of x */
@@ -745,7 +745,8 @@ sc_status_t sparse_conv_combine_rows_backward(const sc_combine_rows_t* d, const 
  * as a sum of 16-bit numbers, 2^-16 (bf16), 2^-22 (f16) or, bf16 with 32-bit results, 2^-24 of it off; y is rounded once.
  * Rows that no group names get base; an index outside 0 .. rows - 1 names none.  Each row may be named once: one that several places
  * name is unspecified.  Offsets out of range are taken as by sparse_conv_matmul_grouped.  Adapters of a smaller rank
- * are filled up with zeros (in a or in b, the other finite). */
+ * are filled up with zeros (in a or in b, the other finite).  What is not finite in x or a makes its rows not finite, in b its column of the group's rows (an
+ * infinity may become a NaN). */
 typedef struct {
     int32_t M, N, K, R, E;       /* M >= 0 places of index; N, K >= 1; 1 <= R <= 256; 1 <= E <= 4096 */
     int32_t rows;                /* rows of x, base and y (without an index: >= M) */

@@ -5,7 +5,7 @@
 // equal logits go by rising number of themselves: 32 bits for 16-bit logits, 64 for 32-bit ones.  With a bias the sums are taken
 // in 64 bits, since scores in 32 bits lie next to one another too often for a choice that has to be repeatable; the expert takes the last twelve of
 // them.  What bounds it is the vector unit: 16384 x 128 logits of 16 bits, top 8 (4096 waves), 11.1 us with comparisons of floats and numbers
-// and the library's exponential and division, 9.6 without, 9.2 with sorted keys (see choose).
+// and the library's exponential and division, 10.7 without, 10.2 with sorted keys (see choose; calls back to back, the kernel alone takes 10.1).
 #include "op_common.h"
 
 #include <cmath>
@@ -122,8 +122,8 @@ template <> struct Key<SC_ELEM_F32> {
 
 // The `top` largest keys of a token's L lanes, one after the other; a lane gets that of its own number, or 0 where there is none.  With eight keys a
 // lane and six choices or more a lane's keys are sorted first (Batcher's merges of odd and even places), so that a choice compares the lanes' largest and one
-// lane moves up; else all are compared for every choice (16384 tokens, us, compared and sorted: 128 experts, bias, top 8 10.2 and 9.5; 64, top 2 4.5 and 5.1; 256,
-// sixteen keys a lane, top 8 12.6 and 16.9; 28936 x 56, bias, top 16 23.8 and 19.5).
+// lane moves up; else all are compared for every choice (16384 tokens, us a call, compared and sorted: 128 experts, bias, top 8 10.7 and 10.2, top 4 8.1 and 8.3; 64, top 2 4.3 and
+// 4.8; 256, sixteen keys a lane, top 8 12.4 and 16.9; 28936 x 56, bias, top 16 24.3 and 19.8; 15376 x 512, top 16 21 and 18, bias 51 and 42).
 template <int L, class T, int V> __device__ __forceinline__ T choose(T (&key)[V], int top, int lane)
 {
     T slot = 0;
